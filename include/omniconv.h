@@ -340,6 +340,74 @@ int omni_dropout_backward(int32_t dtype, int64_t count, float p, uint64_t seed, 
                           const void *dy, void *dx, void *hip_stream);
 
 /*
+ * The end of a network: layer norm, what is read off its logits, and the loss that trains it.  Matrices are [rows][ld] of
+ * `dtype`, of which the first width (classes) elements of a row count, ld >= width; the rest of a row is neither read nor
+ * written, and ld need not be a multiple of anything.  Everything else is dense: fp32 per row or per column, indexes int64.
+ * Arithmetic in fp32, one rounding on store.  An output may be the input named with it below, with the same ld; no other
+ * buffers may overlap.  rows == 0 launches nothing (layer_norm_backward then clears dgamma and dbeta).  A workspace sized for
+ * the most rows serves fewer.
+ *
+ *   layer_norm_forward : mu = mean x, r = (mean (x - mu)^2 + eps)^(-1/2), y = (x - mu) r gamma + beta, over the `width`
+ *       elements of a row (at most 2^28); gamma, beta fp32 [width], nullable (1, 0).  mean, rstd (fp32 [rows], nullable)
+ *       receive mu and r; the backward pass needs them.  y may be x.
+ *   layer_norm_backward: with xh = (x - mu) r, g = dy gamma:  dx = r (g - mean g - xh mean(g xh)),
+ *       dgamma = sum over rows of dy xh, dbeta = sum over rows of dy (fp32 [width], in an order that only the sizes decide).
+ *       dx, dgamma and dbeta are nullable, not all three; without dgamma and dbeta no workspace is needed.  dx may be x or dy.
+ *
+ *   logprob_forward : ln p = z - ln sum exp z, z = (logits - max) / temperature, of a row's classes (at most 2^30).
+ *       logprob [rows][given] receives ln p of the classes targets [rows][given] (given <= 1024; 0: none).  A target below 0
+ *       is left out: 0 here, no gradient.  A target of `classes` or more makes its log probability, and in the backward pass
+ *       its row's gradient, NaN.
+ *       entropy (fp32 [rows], nullable) receives - sum p ln p.
+ *       top_index, top_logprob [rows][top] receive the `top` (0 to 64) largest classes in descending order, equal ones by
+ *       ascending index, and their ln p.  Classes of -inf are nobody's alternatives: -1 and -inf fill what is left.
+ *       stats (fp32 [rows][2], nullable) receives max and sum exp z, which the backward pass needs.
+ *       A class of -inf has probability 0.  A row of nothing else has ln p = -inf for every class, entropy 0 and gradient 0.
+ *       A NaN or +inf among a row's classes makes its results NaN (alternatives: the order of those that are no NaN).
+ *   logprob_backward: dlogits[i] = ( sum_j dlogprob_j ([i = target_j] - p_i) - dentropy p_i (ln p_i + entropy) ) / temperature.
+ *       A class named by several targets receives all of theirs.  dentropy (nullable) needs entropy.  dlogits may be logits.
+ *
+ *   distill_forward : loss [rows] = alpha T^2 sum_k q_k (ln q_k - ln p_k) + (1 - alpha) (- ln p1_label), with T = temperature,
+ *       p = softmax(logits / T), p1 = softmax(logits).  A row's teacher entries are its classes teacher_index [rows][kept] with
+ *       logits (or log probabilities, which differ by a constant) teacher_logits fp32 [rows][kept], kept <= 256, and
+ *       q = softmax(teacher_logits / T) over them: what top_index and top_logprob hold can be handed over as it is.  An entry
+ *       with an index below 0 or a logit of -inf is not there; a row without entries has no first term.  labels (int64
+ *       [rows], nullable): a label below 0, or labels == NULL, leaves the second term out.  kept = 0 with alpha = 0 is the
+ *       plain cross entropy.  An index or label of `classes` or more, and an entry that is NaN or +inf, make the row's loss
+ *       and gradient NaN.  A row with no possible class (all -inf) has loss +inf, where a term is there, and gradient 0.
+ *       stats (fp32 [rows][4], nullable) receives what the backward pass needs.
+ *   distill_backward: dlogits[i] = w ( alpha T (p_i - sum_{k: index_k = i} q_k) + (1 - alpha) (p1_i - [i = label]) ),
+ *       w = scale * dloss[row] (dloss fp32 [rows], nullable: 1), without the terms that the loss is without.  dlogits may be
+ *       logits.
+ *   distill_forward_backward: both, reading a row once from memory.  dlogits may be logits.
+ * The *_workspace_bytes calls are host only; 0 means that workspace may be NULL.
+ */
+int omni_layer_norm_forward(int32_t dtype, int64_t rows, int64_t width, const void *x, int64_t ldx, const float *gamma,
+                            const float *beta, float eps, void *y, int64_t ldy, float *mean, float *rstd, void *hip_stream);
+int omni_layer_norm_workspace_bytes(int32_t dtype, int64_t rows, int64_t width, size_t *bytes);
+int omni_layer_norm_backward(int32_t dtype, int64_t rows, int64_t width, const void *x, int64_t ldx, const void *dy, int64_t lddy,
+                             const float *gamma, const float *mean, const float *rstd, void *dx, int64_t lddx, float *dgamma,
+                             float *dbeta, void *workspace, size_t workspace_bytes, void *hip_stream);
+int omni_logprob_workspace_bytes(int32_t dtype, int64_t rows, int64_t classes, int32_t top, size_t *bytes);
+int omni_logprob_forward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, float temperature,
+                         const int64_t *targets, int32_t given, float *logprob, float *entropy, int32_t top, int64_t *top_index,
+                         float *top_logprob, float *stats, void *workspace, size_t workspace_bytes, void *hip_stream);
+int omni_logprob_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, float temperature,
+                          const float *stats, const int64_t *targets, int32_t given, const float *dlogprob, const float *dentropy,
+                          const float *entropy, void *dlogits, int64_t ld_out, void *hip_stream);
+int omni_distill_workspace_bytes(int32_t dtype, int64_t rows, int64_t classes, size_t *bytes);
+int omni_distill_forward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const int64_t *teacher_index,
+                         const float *teacher_logits, int32_t kept, const int64_t *labels, float temperature, float alpha,
+                         float *loss, float *stats, void *workspace, size_t workspace_bytes, void *hip_stream);
+int omni_distill_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const int64_t *teacher_index,
+                          const float *teacher_logits, int32_t kept, const int64_t *labels, float temperature, float alpha,
+                          const float *stats, const float *dloss, float scale, void *dlogits, int64_t ld_out, void *hip_stream);
+int omni_distill_forward_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld,
+                                  const int64_t *teacher_index, const float *teacher_logits, int32_t kept, const int64_t *labels,
+                                  float temperature, float alpha, const float *dloss, float scale, float *loss, void *dlogits,
+                                  int64_t ld_out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Per-kernel timing (the paper times with a wall clock, App. C "Experiment Setup"; on a GPU the
  * equivalent is an event pair on the stream).  omni_profile_enable(1) clears earlier records and
  * makes every later launch of the library record a start and a stop event on its stream, tagged

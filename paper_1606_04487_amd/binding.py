@@ -35,7 +35,10 @@ SYMBOLS = [
     "omni_maxpool_forward", "omni_maxpool_backward", "omni_maxpool_relu_backward",
     "omni_conv_dy_rows_layout", "omni_relu_backward_rows", "omni_maxpool_backward_rows", "omni_conv_backward_weights_rows",
     "omni_conv_backward_data_rows", "omni_conv_backward_data_relu_rows_sums", "omni_conv_backward_data_relu_rows",
-    "omni_lrn_forward", "omni_lrn_backward", "omni_dropout_forward", "omni_dropout_backward", "omni_status_string", "omni_version", "omni_tuning_set",
+    "omni_lrn_forward", "omni_lrn_backward", "omni_dropout_forward", "omni_dropout_backward",
+    "omni_layer_norm_forward", "omni_layer_norm_workspace_bytes", "omni_layer_norm_backward", "omni_logprob_workspace_bytes",
+    "omni_logprob_forward", "omni_logprob_backward", "omni_distill_workspace_bytes", "omni_distill_forward", "omni_distill_backward",
+    "omni_distill_forward_backward", "omni_status_string", "omni_version", "omni_tuning_set",
     "omni_profile_enable", "omni_profile_select", "omni_profile_select_mask", "omni_profile_kernel_count", "omni_profile_kernel_name", "omni_profile_summary",
 ]
 
@@ -99,7 +102,16 @@ _lib.omni_lrn_forward.argtypes = [_i32, _i64, _i32, _i64, _i32, _f, _f, _f, _vp,
 _lib.omni_lrn_backward.argtypes = [_i32, _i64, _i32, _i64, _i32, _f, _f, _f, _vp, _vp, _vp, _vp, _vp]
 _lib.omni_dropout_forward.argtypes = [_i32, _i64, _f, _u64, _u64, _vp, _vp, _vp]
 _lib.omni_dropout_backward.argtypes = [_i32, _i64, _f, _u64, _u64, _vp, _vp, _vp]
-
+_lib.omni_layer_norm_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _f, _vp, _i64, _vp, _vp, _vp]
+_lib.omni_layer_norm_workspace_bytes.argtypes = [_i32, _i64, _i64, ctypes.POINTER(_sz)]
+_lib.omni_layer_norm_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _sz, _vp]
+_lib.omni_logprob_workspace_bytes.argtypes = [_i32, _i64, _i64, _i32, ctypes.POINTER(_sz)]
+_lib.omni_logprob_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _f, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.omni_logprob_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _f, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _i64, _vp]
+_lib.omni_distill_workspace_bytes.argtypes = [_i32, _i64, _i64, ctypes.POINTER(_sz)]
+_lib.omni_distill_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _vp, _vp, _sz, _vp]
+_lib.omni_distill_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _vp, _f, _vp, _i64, _vp]
+_lib.omni_distill_forward_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _f, _vp, _vp, _i64, _vp, _sz, _vp]
 
 _lib.omni_profile_enable.argtypes = [ctypes.c_int]
 _lib.omni_profile_select_mask.argtypes = [ctypes.c_uint64]
@@ -539,6 +551,233 @@ def dropout_backward(dy, p: float, seed: int, stream_id: int = 0, dx=None):
     dx = torch.empty_like(dy) if dx is None else dx
     _check(_lib.omni_dropout_backward(dtype_code(dy.dtype), dy.numel(), p, seed, stream_id, _p(dy), _p(dx), _stream()))
     return dx
+
+
+# ---------------------------------------------------------------- the end of a network
+# Matrices here are tensors [..., width] whose rows lie evenly spaced, each contiguous: a slice of a wider matrix is one.
+def _matrix(t: torch.Tensor, what: str):
+    """(data_ptr, rows, width, ld) of a tensor on the current GPU."""
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what} must live on the current GPU")
+    if t.dim() == 0 or t.shape[-1] == 0:
+        raise ValueError(f"{what} must have rows of at least one element")
+    width = t.shape[-1]
+    if t.is_contiguous():
+        return t.data_ptr(), t.numel() // width, width, width
+    if width > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    rows, ld = 1, None
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if ld is None:
+            ld = s
+        elif s != ld * rows:
+            raise ValueError(f"{what} must have evenly spaced rows")
+        rows *= n
+    if ld is not None and rows and ld < width:
+        raise ValueError(f"{what} must have rows that do not overlap")
+    return t.data_ptr(), rows, width, width if ld is None else max(ld, width)
+
+
+def _vector(t: Optional[torch.Tensor], count: int, dtype: torch.dtype, what: str) -> Optional[int]:
+    """data_ptr of a dense tensor of `count` elements on the current GPU (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != count:
+        raise ValueError(f"{what} must be {dtype} and hold {count} elements")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device() or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous and live on the current GPU")
+    return t.data_ptr()
+
+
+def _like(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, what: str):
+    p, r, w, ld = _matrix(t, what)
+    if (r, w) != (rows, width) or t.dtype is not dtype:
+        raise ValueError(f"{what} must be {dtype} with {rows} rows of {width}")
+    return p, ld
+
+
+def _scratch(need: int, workspace: Optional[torch.Tensor], device):
+    """(pointer, bytes) of the caller's workspace, or of one that lives until the call returns (the allocator keeps its memory
+    for work queued behind it on the same stream)."""
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace is None:
+        return None, 0, None
+    if not workspace.is_cuda or workspace.get_device() != torch.cuda.current_device() or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and live on the current GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def layer_norm_workspace_bytes(rows: int, width: int, dtype: torch.dtype = torch.float32) -> int:
+    """omni_layer_norm_workspace_bytes: scratch of layer_norm_backward's weight gradients (0: none)."""
+    b = _sz()
+    _check(_lib.omni_layer_norm_workspace_bytes(dtype_code(dtype), rows, width, ctypes.byref(b)))
+    return b.value
+
+
+def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, y=None, mean=None, rstd=None, want_stats: bool = True):
+    """omni_layer_norm_forward over x's last axis; returns (y, mean, rstd) -- mean and rstd (fp32, one a row) are what
+    layer_norm_backward needs (None without want_stats)."""
+    px, rows, width, ldx = _matrix(x, "x")
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
+    py, ldy = _like(y, rows, width, x.dtype, "y")
+    if want_stats:
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
+    f32 = torch.float32
+    _check(_lib.omni_layer_norm_forward(dtype_code(x.dtype), rows, width, px, ldx, _vector(gamma, width, f32, "gamma"),
+                                        _vector(beta, width, f32, "beta"), eps, py, ldy, _vector(mean, rows, f32, "mean"),
+                                        _vector(rstd, rows, f32, "rstd"), _stream()))
+    return y, mean, rstd
+
+
+def layer_norm_backward(x, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, want_dx: bool = True,
+                        want_dweights: bool = True, workspace=None):
+    """omni_layer_norm_backward; returns (dx, dgamma, dbeta), dgamma and dbeta fp32 [width]."""
+    px, rows, width, ldx = _matrix(x, "x")
+    f32, code = torch.float32, dtype_code(x.dtype)
+    pdy, lddy = _like(dy, rows, width, x.dtype, "dy")
+    if dx is None and want_dx:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    pdx, lddx = (None, 0) if dx is None else _like(dx, rows, width, x.dtype, "dx")
+    if want_dweights:
+        dgamma = torch.empty((width,), dtype=f32, device=x.device) if dgamma is None else dgamma
+        dbeta = torch.empty((width,), dtype=f32, device=x.device) if dbeta is None else dbeta
+    need = 0
+    if workspace is None and (dgamma is not None or dbeta is not None):
+        need = layer_norm_workspace_bytes(rows, width, x.dtype)
+    pw, nw, keep = _scratch(need, workspace, x.device)
+    _check(_lib.omni_layer_norm_backward(code, rows, width, px, ldx, pdy, lddy, _vector(gamma, width, f32, "gamma"),
+                                         _vector(mean, rows, f32, "mean"), _vector(rstd, rows, f32, "rstd"), pdx, lddx,
+                                         _vector(dgamma, width, f32, "dgamma"), _vector(dbeta, width, f32, "dbeta"), pw, nw, _stream()))
+    return dx, dgamma, dbeta
+
+
+def logprob_workspace_bytes(rows: int, classes: int, top: int = 0, dtype: torch.dtype = torch.float32) -> int:
+    """omni_logprob_workspace_bytes: scratch of logprob_forward (0: none)."""
+    b = _sz()
+    _check(_lib.omni_logprob_workspace_bytes(dtype_code(dtype), rows, classes, top, ctypes.byref(b)))
+    return b.value
+
+
+def _given(targets, rows: int) -> int:
+    if targets is None:
+        return 0
+    if rows and targets.numel() % rows:
+        raise ValueError("targets must hold the same number of classes for every row")
+    return targets.numel() // rows if rows else 0
+
+
+def logprob_forward(logits, targets=None, top: int = 0, temperature: float = 1.0, logprob=None, entropy=None, top_index=None,
+                    top_logprob=None, stats=None, want_entropy: bool = True, want_stats: bool = True, workspace=None):
+    """omni_logprob_forward over logits [..., classes]; returns (logprob, entropy, top_index, top_logprob, stats).  targets:
+    int64, any number of classes a row; logprob has targets' shape, entropy one value a row, top_index (int64) and top_logprob
+    `top` a row; stats is what logprob_backward needs."""
+    p, rows, classes, ld = _matrix(logits, "logits")
+    f32, i64, dev, lead, code = torch.float32, torch.int64, logits.device, tuple(logits.shape[:-1]), dtype_code(logits.dtype)
+    given = _given(targets, rows)
+    if logprob is None and targets is not None:
+        logprob = torch.empty(targets.shape, dtype=f32, device=dev)
+    if entropy is None and want_entropy:
+        entropy = torch.empty(lead, dtype=f32, device=dev)
+    if top:
+        top_index = torch.empty(lead + (top,), dtype=i64, device=dev) if top_index is None else top_index
+        top_logprob = torch.empty(lead + (top,), dtype=f32, device=dev) if top_logprob is None else top_logprob
+    if stats is None and want_stats:
+        stats = torch.empty(lead + (2,), dtype=f32, device=dev)
+    need = logprob_workspace_bytes(rows, classes, top, logits.dtype) if workspace is None else 0
+    pw, nw, keep = _scratch(need, workspace, dev)
+    _check(_lib.omni_logprob_forward(code, rows, classes, p, ld, temperature, _vector(targets, rows * given, i64, "targets"), given,
+                                     _vector(logprob, rows * given, f32, "logprob"), _vector(entropy, rows, f32, "entropy"), top,
+                                     _vector(top_index, rows * top, i64, "top_index"), _vector(top_logprob, rows * top, f32, "top_logprob"),
+                                     _vector(stats, 2 * rows, f32, "stats"), pw, nw, _stream()))
+    return logprob, entropy, top_index, top_logprob, stats
+
+
+def logprob_backward(logits, stats, targets=None, dlogprob=None, dentropy=None, entropy=None, temperature: float = 1.0, dlogits=None):
+    """omni_logprob_backward: gradient w.r.t. the logits, from dlogprob (targets' shape) and dentropy (one a row, with the
+    entropy that logprob_forward gave)."""
+    p, rows, classes, ld = _matrix(logits, "logits")
+    f32, given = torch.float32, _given(targets, rows)
+    if dlogits is None:
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    po, ldo = _like(dlogits, rows, classes, logits.dtype, "dlogits")
+    _check(_lib.omni_logprob_backward(dtype_code(logits.dtype), rows, classes, p, ld, temperature, _vector(stats, 2 * rows, f32, "stats"),
+                                      _vector(targets, rows * given, torch.int64, "targets"), given,
+                                      _vector(dlogprob, rows * given, f32, "dlogprob"), _vector(dentropy, rows, f32, "dentropy"),
+                                      _vector(entropy, rows, f32, "entropy"), po, ldo, _stream()))
+    return dlogits
+
+
+def distill_workspace_bytes(rows: int, classes: int, dtype: torch.dtype = torch.float32) -> int:
+    """omni_distill_workspace_bytes: scratch of distill_forward and distill_forward_backward (0: none)."""
+    b = _sz()
+    _check(_lib.omni_distill_workspace_bytes(dtype_code(dtype), rows, classes, ctypes.byref(b)))
+    return b.value
+
+
+def _teacher(index, values, labels, rows: int):
+    """(index pointer, logits pointer, entries a row, labels pointer)"""
+    if (index is None) != (values is None):
+        raise ValueError("teacher_index and teacher_logits belong together")
+    kept = 0
+    if index is not None:
+        if index.shape != values.shape or (rows and index.numel() % rows):
+            raise ValueError("teacher_index and teacher_logits must hold the same number of entries for every row")
+        kept = index.numel() // rows if rows else 0
+    return (_vector(index, rows * kept, torch.int64, "teacher_index"), _vector(values, rows * kept, torch.float32, "teacher_logits"), kept,
+            _vector(labels, rows, torch.int64, "labels"))
+
+
+def distill_forward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0, loss=None,
+                    stats=None, want_stats: bool = True, workspace=None):
+    """omni_distill_forward over logits [..., classes]; returns (loss, stats): the loss of every row, and what distill_backward
+    needs.  Without teacher entries (and alpha = 0) it is the labels' cross entropy."""
+    p, rows, classes, ld = _matrix(logits, "logits")
+    f32, dev = torch.float32, logits.device
+    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows)
+    loss = torch.empty(logits.shape[:-1], dtype=f32, device=dev) if loss is None else loss
+    if stats is None and want_stats:
+        stats = torch.empty(tuple(logits.shape[:-1]) + (4,), dtype=f32, device=dev)
+    need = distill_workspace_bytes(rows, classes, logits.dtype) if workspace is None else 0
+    pw, nw, keep = _scratch(need, workspace, dev)
+    _check(_lib.omni_distill_forward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
+                                     _vector(loss, rows, f32, "loss"), _vector(stats, 4 * rows, f32, "stats"), pw, nw, _stream()))
+    return loss, stats
+
+
+def distill_backward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0, stats=None,
+                     dloss=None, scale: float = 1.0, dlogits=None):
+    """omni_distill_backward: gradient w.r.t. the logits of sum(scale * dloss * loss) (dloss: one a row; None: ones)."""
+    p, rows, classes, ld = _matrix(logits, "logits")
+    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows)
+    if dlogits is None:
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    po, ldo = _like(dlogits, rows, classes, logits.dtype, "dlogits")
+    _check(_lib.omni_distill_backward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
+                                      _vector(stats, 4 * rows, torch.float32, "stats"), _vector(dloss, rows, torch.float32, "dloss"), scale,
+                                      po, ldo, _stream()))
+    return dlogits
+
+
+def distill_forward_backward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0,
+                             dloss=None, scale: float = 1.0, loss=None, dlogits=None, workspace=None):
+    """omni_distill_forward_backward: distill_forward and distill_backward in one call; returns (loss, dlogits)."""
+    p, rows, classes, ld = _matrix(logits, "logits")
+    f32, dev = torch.float32, logits.device
+    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows)
+    loss = torch.empty(logits.shape[:-1], dtype=f32, device=dev) if loss is None else loss
+    if dlogits is None:
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    po, ldo = _like(dlogits, rows, classes, logits.dtype, "dlogits")
+    need = distill_workspace_bytes(rows, classes, logits.dtype) if workspace is None else 0
+    pw, nw, keep = _scratch(need, workspace, dev)
+    _check(_lib.omni_distill_forward_backward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
+                                              _vector(dloss, rows, f32, "dloss"), scale, _vector(loss, rows, f32, "loss"), po, ldo, pw, nw,
+                                              _stream()))
+    return loss, dlogits
 
 
 def profile_enable(on: bool) -> None:

@@ -2,6 +2,7 @@
 // Everything before the first launch is plain host code, so every error path can be exercised on a
 // machine without a GPU.
 #include <cmath>
+#include <initializer_list>
 #include <mutex>
 
 #include "common.h"
@@ -990,6 +991,204 @@ int omni_dropout_backward(int32_t dtype, int64_t count, float p, uint64_t seed, 
                           void *hip_stream)
 {
     return dropout_call(dtype, count, p, seed, stream_id, dy, dx, hip_stream);
+}
+
+// ---------------------------------------------------------------- the end of a network
+// A matrix of `rows` rows of `width` elements; the pitches that belong to it are checked by check_pitch.
+static int check_rows(int32_t dtype, int64_t rows, int64_t width, int64_t widest)
+{
+    if (check_dtype(dtype) != OMNI_OK) return OMNI_UNSUPPORTED;
+    if (rows < 0 || width <= 0) return OMNI_INVALID_ARGUMENT;
+    // 32-bit indexes within a row, 2^31 rows, a terabyte and more of elements: what the kernels' grids and indexes take
+    if (width > widest || rows > 0x7fffffffll || (double)rows * (double)width > 1099511627776.0) return OMNI_UNSUPPORTED;
+    return OMNI_OK;
+}
+
+static int check_pitch(int64_t rows, int64_t width, int64_t ld)
+{
+    if (ld < width) return OMNI_INVALID_ARGUMENT;
+    return (double)rows * (double)ld > 4.0e18 / 8.0 ? OMNI_UNSUPPORTED : OMNI_OK;
+}
+
+// an output over an input: the same elements or none
+static bool may_share(const void *out, int64_t ld_out, const void *in, int64_t ld_in) { return out != in || ld_out == ld_in; }
+
+static bool all_aligned16(std::initializer_list<const void *> ps)
+{
+    for (const void *p : ps)
+        if (!aligned16(p)) return false;
+    return true;
+}
+
+static const int64_t NORM_WIDEST = 1 << 28, MOST_CLASSES = 1 << 30;
+
+int omni_layer_norm_forward(int32_t dtype, int64_t rows, int64_t width, const void *x, int64_t ldx, const float *gamma, const float *beta, float eps,
+                            void *y, int64_t ldy, float *mean, float *rstd, void *hip_stream)
+{
+    int st = check_rows(dtype, rows, width, NORM_WIDEST);
+    if (st != OMNI_OK) return st;
+    if (!(eps >= 0.f) || std::isinf(eps)) return OMNI_INVALID_ARGUMENT;
+    if ((st = check_pitch(rows, width, ldx)) != OMNI_OK || (st = check_pitch(rows, width, ldy)) != OMNI_OK) return st;
+    if (rows == 0) return OMNI_OK;
+    if (x == nullptr || y == nullptr || !may_share(y, ldy, x, ldx)) return OMNI_INVALID_ARGUMENT;
+    if (!all_aligned16({x, gamma, beta, y, mean, rstd})) return OMNI_MISALIGNED;
+    return launch_layer_norm_forward(LayerNormArgs{dtype, rows, width, x, ldx, gamma}, eps, beta, y, ldy, mean, rstd, (hipStream_t)hip_stream);
+}
+
+int omni_layer_norm_workspace_bytes(int32_t dtype, int64_t rows, int64_t width, size_t *bytes)
+{
+    if (bytes == nullptr) return OMNI_INVALID_ARGUMENT;
+    int st = check_rows(dtype, rows, width, NORM_WIDEST);
+    if (st != OMNI_OK) return st;
+    *bytes = layer_norm_workspace(dtype, rows, width);
+    return OMNI_OK;
+}
+
+int omni_layer_norm_backward(int32_t dtype, int64_t rows, int64_t width, const void *x, int64_t ldx, const void *dy, int64_t lddy, const float *gamma,
+                             const float *mean, const float *rstd, void *dx, int64_t lddx, float *dgamma, float *dbeta, void *workspace,
+                             size_t workspace_bytes, void *hip_stream)
+{
+    int st = check_rows(dtype, rows, width, NORM_WIDEST);
+    if (st != OMNI_OK) return st;
+    if ((st = check_pitch(rows, width, ldx)) != OMNI_OK || (st = check_pitch(rows, width, lddy)) != OMNI_OK) return st;
+    if (dx != nullptr && (st = check_pitch(rows, width, lddx)) != OMNI_OK) return st;
+    if (dx == nullptr && dgamma == nullptr && dbeta == nullptr) return OMNI_INVALID_ARGUMENT;
+    if (rows > 0 && (x == nullptr || dy == nullptr || mean == nullptr || rstd == nullptr)) return OMNI_INVALID_ARGUMENT;
+    if (dx != nullptr && (!may_share(dx, lddx, x, ldx) || !may_share(dx, lddx, dy, lddy))) return OMNI_INVALID_ARGUMENT;
+    if (!all_aligned16({x, dy, gamma, mean, rstd, dx, dgamma, dbeta, workspace})) return OMNI_MISALIGNED;
+    if (dgamma != nullptr || dbeta != nullptr) {
+        const size_t need = layer_norm_workspace(dtype, rows, width);
+        if (need > 0 && workspace == nullptr) return OMNI_INVALID_ARGUMENT;
+        if (workspace_bytes < need) return OMNI_WORKSPACE_TOO_SMALL;
+    }
+    return launch_layer_norm_backward(LayerNormArgs{dtype, rows, width, x, ldx, gamma}, dy, lddy, mean, rstd, rows > 0 ? dx : nullptr, lddx, dgamma, dbeta,
+                                      (float *)workspace, (hipStream_t)hip_stream);
+}
+
+static int check_logits(int32_t dtype, int64_t rows, int64_t classes, int64_t ld, float temperature)
+{
+    int st = check_rows(dtype, rows, classes, MOST_CLASSES);
+    if (st != OMNI_OK) return st;
+    // 1 / T and log2 e / T are taken in fp32: neither may overflow or vanish
+    if (!(temperature >= 1e-30f) || !(temperature <= 1e30f)) return OMNI_INVALID_ARGUMENT;
+    return check_pitch(rows, classes, ld);
+}
+
+int omni_logprob_workspace_bytes(int32_t dtype, int64_t rows, int64_t classes, int32_t top, size_t *bytes)
+{
+    if (bytes == nullptr || top < 0) return OMNI_INVALID_ARGUMENT;
+    int st = check_rows(dtype, rows, classes, MOST_CLASSES);
+    if (st != OMNI_OK) return st;
+    if (top > TOP_MOST) return OMNI_UNSUPPORTED;
+    *bytes = logprob_workspace(dtype, rows, classes, top);
+    return OMNI_OK;
+}
+
+int omni_logprob_forward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, float temperature, const int64_t *targets,
+                         int32_t given, float *logprob, float *entropy, int32_t top, int64_t *top_index, float *top_logprob, float *stats,
+                         void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    int st = check_logits(dtype, rows, classes, ld, temperature);
+    if (st != OMNI_OK) return st;
+    if (given < 0 || top < 0) return OMNI_INVALID_ARGUMENT;
+    if (given > GIVEN_MOST || top > TOP_MOST) return OMNI_UNSUPPORTED;
+    if (rows == 0) return OMNI_OK;
+    if (logits == nullptr || (given > 0 && (targets == nullptr || logprob == nullptr)) || (top > 0 && (top_index == nullptr || top_logprob == nullptr)))
+        return OMNI_INVALID_ARGUMENT;
+    if (!all_aligned16({logits, targets, logprob, entropy, top_index, top_logprob, stats, workspace})) return OMNI_MISALIGNED;
+    const size_t need = logprob_workspace(dtype, rows, classes, top);
+    if (need > 0 && workspace == nullptr) return OMNI_INVALID_ARGUMENT;
+    if (workspace_bytes < need) return OMNI_WORKSPACE_TOO_SMALL;
+    return launch_logprob_forward(LogitsArgs{dtype, rows, classes, logits, ld, temperature}, targets, given, logprob, entropy, top, top_index, top_logprob,
+                                  stats, workspace, (hipStream_t)hip_stream);
+}
+
+int omni_logprob_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, float temperature, const float *stats,
+                          const int64_t *targets, int32_t given, const float *dlogprob, const float *dentropy, const float *entropy, void *dlogits,
+                          int64_t ld_out, void *hip_stream)
+{
+    int st = check_logits(dtype, rows, classes, ld, temperature);
+    if (st != OMNI_OK || (st = check_pitch(rows, classes, ld_out)) != OMNI_OK) return st;
+    if (given < 0) return OMNI_INVALID_ARGUMENT;
+    if (given > GIVEN_MOST) return OMNI_UNSUPPORTED;
+    if (rows == 0) return OMNI_OK;
+    if (logits == nullptr || stats == nullptr || dlogits == nullptr || (given > 0 && (targets == nullptr || dlogprob == nullptr)) ||
+        (dentropy != nullptr && entropy == nullptr) || !may_share(dlogits, ld_out, logits, ld))
+        return OMNI_INVALID_ARGUMENT;
+    if (!all_aligned16({logits, stats, targets, dlogprob, dentropy, entropy, dlogits})) return OMNI_MISALIGNED;
+    return launch_logprob_backward(LogitsArgs{dtype, rows, classes, logits, ld, temperature}, targets, given, dlogprob, dentropy, entropy, stats, dlogits, ld_out,
+                                   (hipStream_t)hip_stream);
+}
+
+// Checks what the three distillation calls share and fills d; a part of the loss that has no weight is not read.
+static int make_distill(int32_t dtype, int64_t rows, int64_t classes, int64_t ld, const void *logits, const int64_t *teacher_index, const float *teacher_logits,
+                        int32_t kept, const int64_t *labels, float temperature, float alpha, const float *dloss, float scale, DistillArgs *d)
+{
+    int st = check_logits(dtype, rows, classes, ld, temperature);
+    if (st != OMNI_OK) return st;
+    if (kept < 0 || !(alpha >= 0.f) || !(alpha <= 1.f)) return OMNI_INVALID_ARGUMENT;
+    if (kept > KEPT_MOST) return OMNI_UNSUPPORTED;
+    if (temperature < 1e-15f || temperature > 1e15f) return OMNI_INVALID_ARGUMENT;  // the loss has a factor T^2
+    if (rows > 0) {
+        if (logits == nullptr || (kept > 0 && (teacher_index == nullptr || teacher_logits == nullptr))) return OMNI_INVALID_ARGUMENT;
+        if (!(kept > 0 && alpha > 0.f) && !(labels != nullptr && alpha < 1.f)) return OMNI_INVALID_ARGUMENT;  // no loss at all
+        if (!all_aligned16({logits, teacher_index, teacher_logits, labels, dloss})) return OMNI_MISALIGNED;
+    }
+    *d = DistillArgs{teacher_index, teacher_logits, alpha > 0.f ? kept : 0, alpha < 1.f ? labels : nullptr, temperature, alpha, dloss, scale};
+    return OMNI_OK;
+}
+
+int omni_distill_workspace_bytes(int32_t dtype, int64_t rows, int64_t classes, size_t *bytes)
+{
+    if (bytes == nullptr) return OMNI_INVALID_ARGUMENT;
+    int st = check_rows(dtype, rows, classes, MOST_CLASSES);
+    if (st != OMNI_OK) return st;
+    *bytes = distill_workspace(dtype, rows, classes);
+    return OMNI_OK;
+}
+
+static int distill_rows(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const DistillArgs &d, float *loss, float *stats, void *out,
+                        int64_t ld_out, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (loss == nullptr) return OMNI_INVALID_ARGUMENT;
+    if (!all_aligned16({loss, stats, out, workspace})) return OMNI_MISALIGNED;
+    const size_t need = distill_workspace(dtype, rows, classes);
+    if (need > 0 && workspace == nullptr) return OMNI_INVALID_ARGUMENT;
+    if (workspace_bytes < need) return OMNI_WORKSPACE_TOO_SMALL;
+    return launch_distill_rows(LogitsArgs{dtype, rows, classes, logits, ld, d.temperature}, d, loss, stats, out, ld_out, workspace, (hipStream_t)hip_stream);
+}
+
+int omni_distill_forward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const int64_t *teacher_index, const float *teacher_logits,
+                         int32_t kept, const int64_t *labels, float temperature, float alpha, float *loss, float *stats, void *workspace,
+                         size_t workspace_bytes, void *hip_stream)
+{
+    DistillArgs d;
+    int st = make_distill(dtype, rows, classes, ld, logits, teacher_index, teacher_logits, kept, labels, temperature, alpha, nullptr, 1.f, &d);
+    if (st != OMNI_OK || rows == 0) return st;
+    return distill_rows(dtype, rows, classes, logits, ld, d, loss, stats, nullptr, 0, workspace, workspace_bytes, hip_stream);
+}
+
+int omni_distill_forward_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const int64_t *teacher_index,
+                                  const float *teacher_logits, int32_t kept, const int64_t *labels, float temperature, float alpha, const float *dloss,
+                                  float scale, float *loss, void *dlogits, int64_t ld_out, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    DistillArgs d;
+    int st = make_distill(dtype, rows, classes, ld, logits, teacher_index, teacher_logits, kept, labels, temperature, alpha, dloss, scale, &d);
+    if (st != OMNI_OK || (st = check_pitch(rows, classes, ld_out)) != OMNI_OK || rows == 0) return st;
+    if (dlogits == nullptr || !may_share(dlogits, ld_out, logits, ld)) return OMNI_INVALID_ARGUMENT;
+    return distill_rows(dtype, rows, classes, logits, ld, d, loss, nullptr, dlogits, ld_out, workspace, workspace_bytes, hip_stream);
+}
+
+int omni_distill_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const int64_t *teacher_index, const float *teacher_logits,
+                          int32_t kept, const int64_t *labels, float temperature, float alpha, const float *stats, const float *dloss, float scale,
+                          void *dlogits, int64_t ld_out, void *hip_stream)
+{
+    DistillArgs d;
+    int st = make_distill(dtype, rows, classes, ld, logits, teacher_index, teacher_logits, kept, labels, temperature, alpha, dloss, scale, &d);
+    if (st != OMNI_OK || (st = check_pitch(rows, classes, ld_out)) != OMNI_OK || rows == 0) return st;
+    if (stats == nullptr || dlogits == nullptr || !may_share(dlogits, ld_out, logits, ld)) return OMNI_INVALID_ARGUMENT;
+    if (!all_aligned16({stats, dlogits})) return OMNI_MISALIGNED;
+    return launch_distill_backward(LogitsArgs{dtype, rows, classes, logits, ld, temperature}, d, stats, dlogits, ld_out, (hipStream_t)hip_stream);
 }
 
 }  // extern "C"

@@ -136,7 +136,7 @@ inline size_t elem_size(int dtype) { return dtype == OMNI_BF16 ? 2 : 4; }
 enum KernelId {
     KID_LOWER = 0, KID_PACK_KHAT, KID_PACK_DYHAT, KID_BIAS_REDUCE, KID_GEMM_FWD, KID_GEMM_DGRAD, KID_GEMM_WGRAD,
     KID_REDUCE_PARTIALS, KID_COL2IM, KID_SGD, KID_RELU, KID_POOL_FWD, KID_POOL_BWD, KID_FUSED_FWD, KID_FUSED_DGRAD, KID_STRIDED_FWD,
-    KID_LRN, KID_DROPOUT,
+    KID_LRN, KID_DROPOUT, KID_LAYER_NORM, KID_LOGPROB, KID_DISTILL,
     KID_COUNT
 };
 // Brackets the launches made during its lifetime with two events on `s` when profiling is on.
@@ -306,5 +306,26 @@ int launch_lrn(int dtype, bool backward, int64_t N, int32_t C, int64_t plane, in
                const void *x, const void *dy, float *scale, void *out, hipStream_t s);
 int launch_dropout(int dtype, int64_t count, uint32_t threshold, float scale, uint64_t seed, uint64_t stream_id, const void *x,
                    void *y, hipStream_t s);
+
+// layernorm.hip: rows of a matrix [rows][ld], width elements each
+struct LayerNormArgs { int dtype; int64_t rows, width; const void *x; int64_t ldx; const float *gamma; };
+int launch_layer_norm_forward(const LayerNormArgs &a, float eps, const float *beta, void *y, int64_t ldy, float *mean, float *rstd, hipStream_t s);
+size_t layer_norm_workspace(int dtype, int64_t rows, int64_t n);  // of the weights' gradients
+int launch_layer_norm_backward(const LayerNormArgs &a, const void *dy, int64_t lddy, const float *mean, const float *rstd, void *dx, int64_t lddx,
+                               float *dgamma, float *dbeta, float *part, hipStream_t s);
+
+// logits.hip: rows of logits [rows][ld], `classes` elements each
+constexpr int TOP_MOST = 64, GIVEN_MOST = 1024, KEPT_MOST = 256;  // top alternatives, given classes, teacher's entries of a row
+struct LogitsArgs { int dtype; int64_t rows, classes; const void *logits; int64_t ld; float temperature; };
+size_t logprob_workspace(int dtype, int64_t rows, int64_t classes, int top);
+size_t distill_workspace(int dtype, int64_t rows, int64_t classes);
+int launch_logprob_forward(const LogitsArgs &a, const int64_t *targets, int given, float *logprob, float *entropy, int top, int64_t *top_index,
+                           float *top_logprob, float *stats, void *workspace, hipStream_t s);
+int launch_logprob_backward(const LogitsArgs &a, const int64_t *targets, int given, const float *dlogprob, const float *dentropy, const float *entropy,
+                            const float *stats, void *out, int64_t ld_out, hipStream_t s);
+struct DistillArgs { const int64_t *index; const float *teacher; int kept; const int64_t *labels; float temperature, alpha; const float *dloss; float scale; };
+int launch_distill_rows(const LogitsArgs &a, const DistillArgs &d, float *loss, float *stats, void *out, int64_t ld_out, void *workspace,
+                        hipStream_t s);  // out null: the loss alone
+int launch_distill_backward(const LogitsArgs &a, const DistillArgs &d, const float *stats, void *out, int64_t ld_out, hipStream_t s);
 
 }  // namespace omni

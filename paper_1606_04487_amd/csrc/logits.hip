@@ -1,0 +1,612 @@
+// What is read off a network's logits (gfx950): log probabilities of given classes with the entropy and the top
+// alternatives, and the distillation loss, each with its gradient.
+//   z = (x - m) / T, m = max x, s = sum e^z:  ln p_i = z_i - ln s,  H = ln s - sum z e^z / s
+// A row is read once: every thread keeps a running maximum and the sums relative to it, and the threads' are joined.  z is
+// formed as a difference first, so a row of the type's lowest values is a uniform one and not an empty one; a class of -inf
+// has no probability and a row of nothing else none at all (m = -inf, s = 0).  A NaN or +inf makes the row's results NaN.
+#include "row_ops.h"
+
+namespace omni {
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+// z below which e^z is zero; -inf is raised to it where it is multiplied with e^z
+constexpr float Z_LEAST = -16384.f;
+
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }  // one instruction, 1 ulp; results below 2^-126 are zero
+
+// ------------------------------------------------------------------------------------------------ a row's pieces
+// 16-byte chunks that start where memory is aligned: chunk c covers elements [c * V - shift, c * V - shift + V).  Chunks lo to
+// hi - 1 are whole; the elements outside them, at most 2 (V - 1), are taken one a thread.
+template <typename T> struct RowSplit {
+    int shift, lo, hi, head, edges;
+    __device__ __forceinline__ RowSplit(const T *row, int n)
+    {
+        constexpr int V = CHUNK<T>;
+        shift = (int)(((uintptr_t)row / sizeof(T)) % V);
+        lo = shift > 0 ? 1 : 0;
+        hi = (n + shift) / V;
+        if (hi < lo) hi = lo;
+        head = shift > 0 ? V - shift : 0;
+        if (head > n) head = n;
+        const int tail = n + shift - hi * V;
+        edges = head + (tail > 0 && hi * V >= shift && head < n ? tail : 0);
+    }
+    __device__ __forceinline__ int edge(int i, int n) const { return i < head ? i : n - edges + i; }
+    __device__ __forceinline__ int first(int c) const { return c * CHUNK<T> - shift; }
+};
+
+template <typename T> __device__ __forceinline__ void aligned_chunk(const T *row, int at, float (&v)[CHUNK<T>])
+{
+    const uint4 b = *reinterpret_cast<const uint4 *>(row + at);
+    const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+    unpack(w, v);
+}
+
+// ------------------------------------------------------------------------------------------------ running sums
+// s = sum e^z, t = sum z e^z (in powers of two: z is scaled by log2 e / T) relative to m.
+struct Sums { float m, s, t; };
+
+// SUMS: 1 s, 2 s and t, -1 s and, in t's place, the sum at T = 1
+template <int SUMS> __device__ __forceinline__ void rescale(Sums &a, float m, float c, float c1)
+{
+    if (a.m == m) return;
+    if (a.m == -INFINITY) {  // nothing so far (or NaN, which stays)
+        a.m = m;
+        return;
+    }
+    const float d = (a.m - m) * c, f = exp2_fast(d);
+    if (SUMS == 2) a.t = f > 0.f ? (a.t + d * a.s) * f : 0.f;
+    if (SUMS == -1) a.t *= exp2_fast((a.m - m) * c1);
+    a.s *= f;
+    a.m = m;
+}
+
+template <int SUMS, int N> __device__ __forceinline__ void absorb(Sums &a, const float (&x)[N], float c, float c1)
+{
+    float g = x[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) g = fmaxf(g, x[j]);
+    if (g > a.m) rescale<SUMS>(a, g, c, c1);
+    const float m = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float d = x[j] - m, z = d * c, e = exp2_fast(z);
+        a.s += e;
+        if (SUMS == 2) a.t += fmaxf(z, Z_LEAST) * e;
+        if (SUMS == -1) a.t += exp2_fast(d * c1);
+    }
+}
+
+template <int SUMS, int BLOCK> __device__ __forceinline__ void join(Sums &a, float c, float c1, float *lds)
+{
+    float m[1] = {a.m}, v[2];
+    block_join<BLOCK>(m, lds, Max());
+    rescale<SUMS>(a, m[0], c, c1);
+    v[0] = a.s, v[1] = a.t;
+    block_join<BLOCK>(v, lds, Add());
+    a.s = v[0], a.t = v[1];
+}
+
+constexpr int UNROLL = 4;  // chunks a thread loads before it uses the first
+
+// The sums over a row; the thread's own maximum (for the top alternatives) goes to *own.
+template <typename T, int BLOCK, int SUMS> __device__ __forceinline__ Sums row_sums(const T *row, int n, const RowSplit<T> &sp, float c, float c1, float *own, float *lds)
+{
+    constexpr int V = CHUNK<T>;
+    Sums a = {-INFINITY, 0.f, 0.f};
+    const int tid = threadIdx.x;
+    int at = sp.lo;
+    for (; at + UNROLL * BLOCK <= sp.hi; at += UNROLL * BLOCK) {
+        float x[UNROLL][V];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) aligned_chunk(row, sp.first(at + u * BLOCK + tid), x[u]);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) absorb<SUMS>(a, x[u], c, c1);
+    }
+    if (at < sp.hi) {  // the last chunks: loads past them repeat the last one and count as -inf
+        float x[UNROLL][V];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int k = at + u * BLOCK + tid;
+            aligned_chunk(row, sp.first(k < sp.hi ? k : sp.hi - 1), x[u]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[u][j] = k < sp.hi ? x[u][j] : -INFINITY;
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) absorb<SUMS>(a, x[u], c, c1);
+    }
+    if (tid < sp.edges) {
+        const float x[1] = {element(row + sp.edge(tid, n))};
+        absorb<SUMS>(a, x, c, c1);
+    }
+    if (own != nullptr) *own = a.m;
+    join<SUMS, BLOCK>(a, c, c1, lds);
+    return a;
+}
+
+// ------------------------------------------------------------------------------------------------ top alternatives
+// Values in the order of whole numbers (-0 counts as 0), with the index below: larger key = larger value, then lower index.
+__device__ __forceinline__ uint32_t ordered(float v)
+{
+    const uint32_t b = __float_as_uint(v + 0.f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float((int32_t)k < 0 ? k & 0x7fffffffu : ~k); }
+constexpr uint32_t ORDERED_NOTHING = 0x007fffffu;  // ordered(-inf)
+
+constexpr int TOP_KEYS = 512;
+
+struct TopLds {
+    uint64_t keys[TOP_KEYS];
+    uint64_t bar;
+    float group[64];
+    int count, threads;
+    uint16_t thread[1024];
+};
+
+// The k largest of a row, k <= 64, in order.  The k-th largest of 64 groups' maxima is a lower bound of the k-th largest
+// element; the elements that reach it are collected (few more than k) and ranked by comparing each with all.  Only threads whose
+// own maximum reaches the bound can hold one, so only those threads' chunks are read a second time, one such thread's chunks by
+// all lanes of a wavefront.  When more elements reach the bound than there is room for (equal or oddly placed values), the k-th
+// largest of those collected is a higher bound, and the collection is done again: every key is different, so this ends.
+template <typename T, int BLOCK>
+__device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &sp, float own, int k, float m, float inv_t, float lns, int64_t *index, float *lp, TopLds &t)
+{
+    constexpr int V = CHUNK<T>, WAVES = BLOCK / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    // groups of WAVES threads of one wavefront each: 64 / WAVES groups a wavefront
+    float g = own;
+#pragma unroll
+    for (int off = 1; off < WAVES; off *= 2) g = fmaxf(g, __shfl_xor(g, off, 64));
+    if (tid == 0) t.threads = 0;
+    if (lane % WAVES == 0) t.group[wave * (64 / WAVES) + lane / WAVES] = g;
+    __syncthreads();
+    const uint32_t u = ordered(t.group[lane]);
+    uint32_t bound = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t more = bound | (1u << bit);
+        if (__popcll(__ballot(u >= more)) >= k) bound = more;
+    }
+    if (bound <= ORDERED_NOTHING) bound = ORDERED_NOTHING + 1;  // -inf is nobody's alternative
+    if (ordered(own) >= bound && own > -INFINITY) t.thread[atomicAdd(&t.threads, 1)] = (uint16_t)tid;
+    uint64_t bar = (uint64_t)bound << 32;
+    int found;
+    for (;;) {
+        __syncthreads();
+        if (tid == 0) t.count = 0;
+        __syncthreads();
+        auto offer = [&](float x, int i) {
+            const uint64_t key = ((uint64_t)ordered(x) << 32) | (uint32_t)~i;
+            if (key >= bar && x > -INFINITY) {  // (NaN is not)
+                const int to = atomicAdd(&t.count, 1);
+                if (to < TOP_KEYS) t.keys[to] = key;
+            }
+        };
+        for (int a = wave; a < t.threads; a += WAVES) {
+            const int who = t.thread[a];
+            for (int c = sp.lo + who + lane * BLOCK; c < sp.hi; c += 64 * BLOCK) {
+                float x[V];
+                aligned_chunk(row, sp.first(c), x);
+#pragma unroll
+                for (int j = 0; j < V; ++j) offer(x[j], sp.first(c) + j);
+            }
+            if (lane == 0 && who < sp.edges) offer(element(row + sp.edge(who, n)), sp.edge(who, n));
+        }
+        __syncthreads();
+        found = t.count;
+        if (found <= TOP_KEYS) break;
+        for (int i = tid; i < TOP_KEYS; i += BLOCK) {
+            int above = 0;
+            for (int j = 0; j < TOP_KEYS; ++j) above += t.keys[j] > t.keys[i];
+            if (above == k - 1) t.bar = t.keys[i];
+        }
+        __syncthreads();
+        bar = t.bar;
+    }
+    for (int i = tid; i < found; i += BLOCK) {
+        const uint64_t key = t.keys[i];
+        int above = 0;
+        for (int j = 0; j < found; ++j) above += t.keys[j] > key;
+        if (above < k) {
+            index[above] = (int64_t)(uint32_t)~(uint32_t)key;
+            lp[above] = (unordered((uint32_t)(key >> 32)) - m) * inv_t - lns;
+        }
+    }
+    for (int i = found + tid; i < k; i += BLOCK) {
+        index[i] = -1;
+        lp[i] = -INFINITY;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ log probabilities
+template <typename T, int BLOCK, bool ENTROPY>
+__global__ __launch_bounds__(BLOCK) void logprob_forward_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int n, float c, float inv_t,
+                                                                const int64_t *__restrict__ targets, int given, float *__restrict__ logprob, float *__restrict__ entropy,
+                                                                int top, int64_t *__restrict__ top_index, float *__restrict__ top_logprob, float *__restrict__ stats)
+{
+    __shared__ float lds[2 * (BLOCK / 64)];
+    __shared__ TopLds tl;
+    const int64_t r = grid_row();
+    if (r >= rows) return;
+    const T *row = logits + r * ld;
+    const RowSplit<T> sp(row, n);
+    float own;
+    const Sums a = row_sums<T, BLOCK, ENTROPY ? 2 : 1>(row, n, sp, c, 0.f, &own, lds);
+    const float lns = logf(a.s);
+    if (threadIdx.x == 0) {
+        if (ENTROPY) entropy[r] = a.m == -INFINITY && a.s == 0.f ? 0.f : lns - LN2 * a.t / a.s;
+        if (stats != nullptr) stats[2 * r] = a.m, stats[2 * r + 1] = a.s;
+    }
+    for (int i = threadIdx.x; i < given; i += BLOCK) {
+        const int64_t at = targets[r * given + i];
+        float v = at < 0 ? 0.f : NAN;
+        if (at >= 0 && at < n) v = a.m == -INFINITY && a.s == 0.f ? -INFINITY : (element(row + at) - a.m) * inv_t - lns;
+        logprob[r * given + i] = v;
+    }
+    if (top > 0) row_top<T, BLOCK>(row, n, sp, own, top, a.m, inv_t, lns, top_index + r * top, top_logprob + r * top, tl);
+}
+
+// ------------------------------------------------------------------------------------------------ gradients
+// A row's gradient is a function of the element and the row's sums everywhere but at a few listed classes, where something is
+// added.  `value` gives the first; the listed classes are written last, each with all that is added to it in one rounding, by
+// the first entry of the list that names it.  out may be the logits themselves.
+template <int MOST> struct ListLds {
+    int64_t at[MOST];
+    float add[MOST];
+};
+
+// Elements [begin, end) of a row, both multiples of the chunk: the chunks are aligned as the output's row is.
+template <typename T, int BLOCK, typename F> __device__ __forceinline__ void write_row(const T *in, T *out, int n, int64_t c0, int64_t c1, F value)
+{
+    constexpr int V = CHUNK<T>;
+    const int shift = (int)(((uintptr_t)out / sizeof(T)) % V);
+    for (int64_t c = c0 + threadIdx.x; c < c1; c += BLOCK) {
+        const int at = (int)(c * V) - shift;
+        float x[V];
+        load_chunk(in, at, n, 0.f, x);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = value(x[j]);
+        store_chunk(out, at, n, x);
+    }
+}
+
+// The listed classes in the elements that a call of write_row with the same chunks covers: their logits (before), their values
+// (after, with a barrier between).
+template <typename T, int BLOCK, int MOST> struct ListedOut {
+    static constexpr int EACH = (MOST + BLOCK - 1) / BLOCK;
+    float x[EACH];
+    int from, to;
+    __device__ __forceinline__ void read(const T *in, const T *out, int n, int64_t c0, int64_t c1, const ListLds<MOST> &l, int count)
+    {
+        constexpr int V = CHUNK<T>;
+        const int shift = (int)(((uintptr_t)out / sizeof(T)) % V);
+        from = c0 == 0 ? 0 : (int)(c0 * V) - shift;
+        to = c1 * V - shift < n ? (int)(c1 * V) - shift : n;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int i = threadIdx.x + e * BLOCK;
+            if (i < count && l.at[i] >= from && l.at[i] < to) x[e] = element(in + l.at[i]);
+        }
+    }
+    template <typename F> __device__ __forceinline__ void write(T *out, const ListLds<MOST> &l, int count, F value)
+    {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int i = threadIdx.x + e * BLOCK;
+            if (i >= count || l.at[i] < from || l.at[i] >= to) continue;
+            bool first = true;
+            float add = 0.f;
+            for (int j = 0; j < count; ++j)
+                if (l.at[j] == l.at[i]) {
+                    if (j < i) first = false;
+                    add += l.add[j];
+                }
+            if (first) set_element(out + l.at[i], value(x[e]) + add);
+        }
+    }
+};
+
+constexpr int GRAD_BLOCK = 256, GRAD_CHUNKS = 4 * GRAD_BLOCK;  // chunks of a row that a workgroup writes
+
+template <typename T>
+__global__ __launch_bounds__(GRAD_BLOCK) void logprob_backward_kernel(const T *logits, int64_t ld, int64_t rows, int n, int pieces, float c, float inv_t,
+                                                                      const int64_t *__restrict__ targets, int given, const float *__restrict__ dlogprob,
+                                                                      const float *__restrict__ dentropy, const float *__restrict__ entropy, const float *__restrict__ stats,
+                                                                      T *out, int64_t ld_out)
+{
+    __shared__ ListLds<GIVEN_MOST> l;
+    const int64_t id = grid_row(), r = id / pieces;
+    if (r >= rows) return;
+    const int64_t c0 = (id % pieces) * GRAD_CHUNKS, c1 = c0 + GRAD_CHUNKS;
+    const T *in = logits + r * ld;
+    T *to = out + r * ld_out;
+    const float m = stats[2 * r], s = stats[2 * r + 1];
+    const bool none = m == -INFINITY && s == 0.f;
+    for (int i = threadIdx.x; i < given; i += GRAD_BLOCK) {
+        const int64_t at = targets[r * given + i];
+        l.at[i] = at;
+        l.add[i] = at < 0 || none ? 0.f : at < n ? dlogprob[r * given + i] * inv_t : NAN;
+    }
+    __syncthreads();
+    float all = 0.f;
+    for (int i = 0; i < given; ++i) all += l.add[i];
+    // d x = 1/T [ sum dlp (delta - p) - dH p (ln p + H) ] = listed + p (a + b z),  ln p = ln2 z - ln s
+    const float dh = dentropy != nullptr ? dentropy[r] * inv_t : 0.f, lns = logf(s);
+    const float h = dentropy != nullptr ? entropy[r] : 0.f;
+    const float inv_s = none ? 0.f : 1.f / s, a = none ? 0.f : (-all - dh * (h - lns)) * inv_s, b = none ? 0.f : -dh * LN2 * inv_s, m0 = none ? 0.f : m;
+    auto value = [&](float x) {
+        const float z = fmaxf((x - m0) * c, Z_LEAST);
+        return exp2_fast(z) * (a + b * z);
+    };
+    ListedOut<T, GRAD_BLOCK, GIVEN_MOST> listed;
+    listed.read(in, to, n, c0, c1, l, given);
+    __syncthreads();
+    write_row<T, GRAD_BLOCK>(in, to, n, c0, c1, value);
+    __syncthreads();
+    listed.write(to, l, given, value);
+}
+
+template <typename T> static int logprob_backward(const LogitsArgs &a, const int64_t *targets, int given, const float *dlogprob, const float *dentropy, const float *entropy,
+                                                  const float *stats, T *out, int64_t ld_out, hipStream_t s)
+{
+    // one chunk more than the row has: its chunks are counted from an aligned address in front of it
+    const int pieces = (int)(((a.classes + CHUNK<T> - 1) / CHUNK<T> + 1 + GRAD_CHUNKS - 1) / GRAD_CHUNKS);
+    hipLaunchKernelGGL(logprob_backward_kernel<T>, row_grid(a.rows * pieces), dim3(GRAD_BLOCK), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces,
+                       LOG2E / a.temperature, 1.f / a.temperature, targets, given, dlogprob, dentropy, entropy, stats, out, ld_out);
+    OMNI_LAUNCH_CHECK();
+    return OMNI_OK;
+}
+
+int launch_logprob_backward(const LogitsArgs &a, const int64_t *targets, int given, const float *dlogprob, const float *dentropy, const float *entropy, const float *stats,
+                            void *out, int64_t ld_out, hipStream_t s)
+{
+    ProfScope prof(KID_LOGPROB, s, 0.0, 2.0 * (double)a.rows * a.classes * elem_size(a.dtype));
+    return a.dtype == OMNI_BF16 ? logprob_backward<bf16_t>(a, targets, given, dlogprob, dentropy, entropy, stats, (bf16_t *)out, ld_out, s)
+                                : logprob_backward<float>(a, targets, given, dlogprob, dentropy, entropy, stats, (float *)out, ld_out, s);
+}
+
+size_t logprob_workspace(int, int64_t, int64_t, int) { return 0; }
+size_t distill_workspace(int, int64_t, int64_t) { return 0; }
+
+// Threads per row: one wavefront for short rows, so that many rows share a compute unit without barriers; 1024 where the
+// rows are too few to occupy the chip otherwise.
+static int row_block(const LogitsArgs &a)
+{
+    const int64_t chunks = a.classes * (int64_t)elem_size(a.dtype) / 16;
+    if (chunks <= 256) return 64;
+    return a.rows < 512 && chunks > 1024 ? 1024 : 256;
+}
+
+#define OMNI_BY_TYPE_AND_BLOCK(LAUNCH)              \
+    do {                                            \
+        const int block = row_block(a);             \
+        if (a.dtype == OMNI_BF16) {                 \
+            if (block == 64) LAUNCH(bf16_t, 64);    \
+            else if (block == 256) LAUNCH(bf16_t, 256); \
+            else LAUNCH(bf16_t, 1024);              \
+        } else {                                    \
+            if (block == 64) LAUNCH(float, 64);     \
+            else if (block == 256) LAUNCH(float, 256); \
+            else LAUNCH(float, 1024);               \
+        }                                           \
+    } while (0)
+
+int launch_logprob_forward(const LogitsArgs &a, const int64_t *targets, int given, float *logprob, float *entropy, int top, int64_t *top_index, float *top_logprob,
+                           float *stats, void *, hipStream_t s)
+{
+    ProfScope prof(KID_LOGPROB, s, 0.0, (double)a.rows * a.classes * elem_size(a.dtype));
+    const float inv_t = 1.f / a.temperature, c = LOG2E / a.temperature;
+#define OMNI_LOGPROB(T, B)                                                                                                                                          \
+    do {                                                                                                                                                            \
+        if (entropy != nullptr)                                                                                                                                     \
+            hipLaunchKernelGGL((logprob_forward_kernel<T, B, true>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, c, inv_t, targets, \
+                               given, logprob, entropy, top, top_index, top_logprob, stats);                                                                        \
+        else                                                                                                                                                        \
+            hipLaunchKernelGGL((logprob_forward_kernel<T, B, false>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, c, inv_t, targets, \
+                               given, logprob, entropy, top, top_index, top_logprob, stats);                                                                        \
+    } while (0)
+    OMNI_BY_TYPE_AND_BLOCK(OMNI_LOGPROB);
+#undef OMNI_LOGPROB
+    OMNI_LAUNCH_CHECK();
+    return OMNI_OK;
+}
+
+// ------------------------------------------------------------------------------------------------ distillation
+//   q = softmax(t_k / T) over the entries that are there, p = softmax(x / T), p1 = softmax(x)
+//   loss = alpha T^2 sum_k q_k (ln q_k - ln p_{i_k}) + (1 - alpha) (-ln p1_label)
+//   d x_i = w [ alpha T (p_i - sum_{i_k = i} q_k) + (1 - alpha) (p1_i - [i = label]) ]
+// With alpha = 1 or T = 1 one exponential an element serves both softmaxes, else two (TWO).
+typedef ListLds<KEPT_MOST + 1> EntryLds;  // the label behind the entries
+
+// The row's entries: at[k], and q_k in add[k].  Returns {ln sum, max, entries that are there, an index out of range}.
+struct Entries { float lnsum, max; bool any, bad; };  // bad: an index or a logit that makes the row's results NaN
+
+template <int BLOCK> __device__ __forceinline__ Entries read_entries(const DistillArgs &d, int64_t r, int n, float inv_t, EntryLds &l, float *lds)
+{
+    Entries e = {0.f, 0.f, false, false};
+    float v[2] = {-INFINITY, 0.f};
+    for (int i = threadIdx.x; i < d.kept; i += BLOCK) {
+        int64_t at = d.index[r * d.kept + i];
+        const float t = d.teacher[r * d.kept + i];
+        if (t == -INFINITY) at = -1;
+        if (at >= n) v[1] = 1.f;
+        if (at >= 0 && !(t < INFINITY)) v[1] = 1.f;
+        if (at >= 0) v[0] = fmaxf(v[0], t);
+        l.at[i] = at;
+        l.add[i] = t;
+    }
+    block_join<BLOCK>(v, lds, Max());
+    e.max = v[0];
+    e.bad = v[1] > 0.f;
+    e.any = v[0] > -INFINITY;
+    float s[1] = {0.f};
+    for (int i = threadIdx.x; i < d.kept; i += BLOCK)
+        if (l.at[i] >= 0) s[0] += exp2_fast((l.add[i] - e.max) * (inv_t * LOG2E));
+    block_join<BLOCK>(s, lds, Add());
+    e.lnsum = logf(s[0]);
+    return e;
+}
+
+template <typename T, int BLOCK, bool TWO>
+__device__ __forceinline__ float row_loss(const DistillArgs &d, const T *row, int64_t r, int n, const Sums &a, const Entries &e, const EntryLds &l, float *lds)
+{
+    // (TWO: a.s at T, a.t at 1; else a.s for whichever is used)
+    const float inv_t = 1.f / d.temperature;
+    const bool none = a.m == -INFINITY && a.s == 0.f;
+    float sum[1] = {0.f};
+    if (e.any) {
+        // T ln q and T ln p, which stay in range where ln p itself would not (a class masked with the type's lowest value, T < 1)
+        const float tlns = d.temperature * logf(a.s), tlnsum = d.temperature * e.lnsum;
+        for (int i = threadIdx.x; i < d.kept; i += BLOCK) {
+            if (l.at[i] < 0 || l.at[i] >= n) continue;
+            const float lnq = l.add[i] - e.max - tlnsum, q = exp2_fast(lnq * (inv_t * LOG2E));
+            const float lnp = none ? -INFINITY : element(row + l.at[i]) - a.m - tlns;
+            if (!(q == 0.f)) sum[0] += q * (lnq - lnp);
+        }
+        block_join<BLOCK>(sum, lds, Add());
+    }
+    float loss = d.alpha > 0.f && d.kept > 0 ? d.alpha * d.temperature * sum[0] : 0.f;
+    if (e.bad) loss = NAN;
+    if (d.labels != nullptr && d.alpha < 1.f) {
+        const int64_t at = d.labels[r];
+        const float lns1 = logf(TWO ? a.t : a.s);
+        if (at >= n) loss = NAN;
+        else if (at >= 0) loss += (1.f - d.alpha) * (none ? INFINITY : lns1 - (element(row + at) - a.m));
+    }
+    return loss;
+}
+
+// The gradient's coefficients: d x = cT 2^(zT) + c1 2^(z1) + what is listed (entries, then the label).
+struct Coefs { float ct, c1; int count; };
+
+template <int BLOCK, bool TWO> __device__ __forceinline__ Coefs row_coefs(const DistillArgs &d, int64_t r, int n, float m, float s, float s1, const Entries &e, float w, EntryLds &l)
+{
+    const float inv_t = 1.f / d.temperature, soft = d.alpha * d.temperature * w, hard = (1.f - d.alpha) * w;
+    const bool none = m == -INFINITY && s == 0.f;
+    Coefs k = {0.f, 0.f, d.kept};
+    for (int i = threadIdx.x; i < d.kept; i += BLOCK)
+        l.add[i] = none || l.at[i] < 0 ? 0.f : -soft * exp2_fast(((l.add[i] - e.max) * inv_t - e.lnsum) * LOG2E);
+    if (e.any && !none) k.ct = soft / s;
+    if (e.bad) k.ct = NAN;
+    if (d.labels != nullptr && d.alpha < 1.f) {
+        const int64_t at = d.labels[r];
+        if (threadIdx.x == 0) {
+            l.at[d.kept] = at < n ? at : -1;
+            l.add[d.kept] = none ? 0.f : -hard;
+        }
+        ++k.count;
+        if (at >= 0 && !none) k.c1 = hard / (TWO ? s1 : s);
+        if (at >= n) k.c1 = NAN;
+    }
+    __syncthreads();
+    return k;
+}
+
+// Whole rows: the loss, and with GRADIENT also the gradient, for which the row is read again while the caches hold it.
+template <typename T, int BLOCK, bool TWO, bool GRADIENT>
+__global__ __launch_bounds__(BLOCK) void distill_rows_kernel(const T *logits, int64_t ld, int64_t rows, int n, DistillArgs d, float *__restrict__ loss,
+                                                             float *__restrict__ stats, T *out, int64_t ld_out)
+{
+    __shared__ float lds[2 * (BLOCK / 64)];
+    __shared__ EntryLds l;
+    const int64_t r = grid_row();
+    if (r >= rows) return;
+    const T *row = logits + r * ld;
+    const RowSplit<T> sp(row, n);
+    const float t = d.alpha > 0.f && d.kept > 0 ? d.temperature : 1.f, c = LOG2E / t;
+    const Sums a = row_sums<T, BLOCK, TWO ? -1 : 1>(row, n, sp, c, LOG2E, nullptr, lds);
+    const Entries e = read_entries<BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
+    __syncthreads();
+    const float v = row_loss<T, BLOCK, TWO>(d, row, r, n, a, e, l, lds);
+    if (threadIdx.x == 0) {
+        if (loss != nullptr) loss[r] = v;
+        if (stats != nullptr) stats[4 * r] = a.m, stats[4 * r + 1] = a.s, stats[4 * r + 2] = TWO ? a.t : a.s, stats[4 * r + 3] = 0.f;
+    }
+    if (!GRADIENT) return;
+    T *to = out + r * ld_out;
+    const Coefs k = row_coefs<BLOCK, TWO>(d, r, n, a.m, a.s, a.t, e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
+    const float m0 = a.m == -INFINITY ? 0.f : a.m, ct = TWO ? k.ct : k.ct + k.c1;
+    auto value = [&](float x) {
+        const float z = x - m0;
+        return TWO ? exp2_fast(z * c) * ct + exp2_fast(z * LOG2E) * k.c1 : exp2_fast(z * c) * ct;
+    };
+    ListedOut<T, BLOCK, KEPT_MOST + 1> listed;
+    const int64_t chunks = (n + CHUNK<T> - 1) / CHUNK<T> + 1;
+    listed.read(row, to, n, 0, chunks, l, k.count);
+    __syncthreads();
+    write_row<T, BLOCK>(row, to, n, 0, chunks, value);
+    __syncthreads();
+    listed.write(to, l, k.count, value);
+}
+
+template <typename T, bool TWO>
+__global__ __launch_bounds__(GRAD_BLOCK) void distill_backward_kernel(const T *logits, int64_t ld, int64_t rows, int n, int pieces, DistillArgs d,
+                                                                      const float *__restrict__ stats, T *out, int64_t ld_out)
+{
+    __shared__ float lds[2 * (GRAD_BLOCK / 64)];
+    __shared__ EntryLds l;
+    const int64_t id = grid_row(), r = id / pieces;
+    if (r >= rows) return;
+    const int64_t c0 = (id % pieces) * GRAD_CHUNKS, c1 = c0 + GRAD_CHUNKS;
+    const T *in = logits + r * ld;
+    T *to = out + r * ld_out;
+    const float t = d.alpha > 0.f && d.kept > 0 ? d.temperature : 1.f, c = LOG2E / t, m = stats[4 * r];
+    const Entries e = read_entries<GRAD_BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
+    __syncthreads();
+    const Coefs k = row_coefs<GRAD_BLOCK, TWO>(d, r, n, m, stats[4 * r + 1], stats[4 * r + 2], e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
+    const float m0 = m == -INFINITY ? 0.f : m, ct = TWO ? k.ct : k.ct + k.c1;
+    auto value = [&](float x) {
+        const float z = x - m0;
+        return TWO ? exp2_fast(z * c) * ct + exp2_fast(z * LOG2E) * k.c1 : exp2_fast(z * c) * ct;
+    };
+    ListedOut<T, GRAD_BLOCK, KEPT_MOST + 1> listed;
+    listed.read(in, to, n, c0, c1, l, k.count);
+    __syncthreads();
+    write_row<T, GRAD_BLOCK>(in, to, n, c0, c1, value);
+    __syncthreads();
+    listed.write(to, l, k.count, value);
+}
+
+// two exponentials an element: both losses are there, at different temperatures
+static bool two_softmaxes(const DistillArgs &d) { return d.alpha > 0.f && d.alpha < 1.f && d.kept > 0 && d.labels != nullptr && d.temperature != 1.f; }
+
+int launch_distill_rows(const LogitsArgs &a, const DistillArgs &d, float *loss, float *stats, void *out, int64_t ld_out, void *, hipStream_t s)
+{
+    ProfScope prof(KID_DISTILL, s, 0.0, (out != nullptr ? 2.0 : 1.0) * (double)a.rows * a.classes * elem_size(a.dtype));
+    const bool two = two_softmaxes(d);
+#define OMNI_DISTILL_ROWS(T, B, TWO, G) \
+    hipLaunchKernelGGL((distill_rows_kernel<T, B, TWO, G>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, d, loss, stats, (T *)out, ld_out)
+#define OMNI_DISTILL(T, B)                                                    \
+    do {                                                                      \
+        if (two && out != nullptr) OMNI_DISTILL_ROWS(T, B, true, true);       \
+        else if (two) OMNI_DISTILL_ROWS(T, B, true, false);                   \
+        else if (out != nullptr) OMNI_DISTILL_ROWS(T, B, false, true);        \
+        else OMNI_DISTILL_ROWS(T, B, false, false);                           \
+    } while (0)
+    OMNI_BY_TYPE_AND_BLOCK(OMNI_DISTILL);
+#undef OMNI_DISTILL
+#undef OMNI_DISTILL_ROWS
+    OMNI_LAUNCH_CHECK();
+    return OMNI_OK;
+}
+
+template <typename T> static int distill_backward(const LogitsArgs &a, const DistillArgs &d, const float *stats, T *out, int64_t ld_out, hipStream_t s)
+{
+    const int pieces = (int)(((a.classes + CHUNK<T> - 1) / CHUNK<T> + 1 + GRAD_CHUNKS - 1) / GRAD_CHUNKS);
+    if (two_softmaxes(d))
+        hipLaunchKernelGGL((distill_backward_kernel<T, true>), row_grid(a.rows * pieces), dim3(GRAD_BLOCK), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, d, stats,
+                           out, ld_out);
+    else
+        hipLaunchKernelGGL((distill_backward_kernel<T, false>), row_grid(a.rows * pieces), dim3(GRAD_BLOCK), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, d, stats,
+                           out, ld_out);
+    OMNI_LAUNCH_CHECK();
+    return OMNI_OK;
+}
+
+int launch_distill_backward(const LogitsArgs &a, const DistillArgs &d, const float *stats, void *out, int64_t ld_out, hipStream_t s)
+{
+    ProfScope prof(KID_DISTILL, s, 0.0, 2.0 * (double)a.rows * a.classes * elem_size(a.dtype));
+    return a.dtype == OMNI_BF16 ? distill_backward<bf16_t>(a, d, stats, (bf16_t *)out, ld_out, s) : distill_backward<float>(a, d, stats, (float *)out, ld_out, s);
+}
+
+}  // namespace omni

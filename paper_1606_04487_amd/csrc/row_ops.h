@@ -1,0 +1,115 @@
+// Device helpers of the kernels that walk the rows of a matrix (layernorm.hip, logits.hip): a row of n elements is read in
+// chunks of 16 bytes, a workgroup works on one row or on a piece of one, and its sums are joined in a fixed order.
+#pragma once
+
+#include "common.h"
+
+namespace omni {
+
+// elements of a 16-byte chunk
+template <typename T> constexpr int CHUNK = 16 / (int)sizeof(T);
+
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) ChunkBits { uint32_t w[4]; };  // of any element alignment
+
+__device__ __forceinline__ void unpack(const uint32_t (&w)[4], float (&v)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[2 * j] = __uint_as_float(w[j] << 16);
+        v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void unpack(const uint32_t (&w)[4], float (&v)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(w[j]);
+}
+__device__ __forceinline__ void pack(const float (&v)[8], uint32_t (&w)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = f32x2_to_bf16x2(v[2 * j], v[2 * j + 1]);
+}
+__device__ __forceinline__ void pack(const float (&v)[4], uint32_t (&w)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(v[j]);
+}
+
+__device__ __forceinline__ float element(const float *p) { return *p; }
+__device__ __forceinline__ float element(const bf16_t *p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ void set_element(float *p, float v) { *p = v; }
+__device__ __forceinline__ void set_element(bf16_t *p, float v) { *p = f32_to_bf16(v); }
+
+// Elements [at, at + CHUNK) of a row of n; those outside it are `fill`.
+template <typename T> __device__ __forceinline__ void load_chunk(const T *row, int at, int n, float fill, float (&v)[CHUNK<T>])
+{
+    if (at >= 0 && at + CHUNK<T> <= n) {
+        const ChunkBits<T> b = *reinterpret_cast<const ChunkBits<T> *>(row + at);
+        unpack(b.w, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < CHUNK<T>; ++j) v[j] = at + j >= 0 && at + j < n ? element(row + at + j) : fill;
+    }
+}
+template <typename T> __device__ __forceinline__ void store_chunk(T *row, int at, int n, const float (&v)[CHUNK<T>])
+{
+    if (at >= 0 && at + CHUNK<T> <= n) {
+        ChunkBits<T> b;
+        pack(v, b.w);
+        *reinterpret_cast<ChunkBits<T> *>(row + at) = b;
+    } else {
+#pragma unroll
+        for (int j = 0; j < CHUNK<T>; ++j)
+            if (at + j >= 0 && at + j < n) set_element(row + at + j, v[j]);
+    }
+}
+
+// ---------------------------------------------------------------- one workgroup per row
+// Rows run over a grid's x and then its y: 2^20 workgroups of 1024 threads are what x takes.
+constexpr int64_t ROW_GRID = 1 << 20;
+inline dim3 row_grid(int64_t rows) { return dim3((unsigned)(rows < ROW_GRID ? rows : ROW_GRID), (unsigned)((rows + ROW_GRID - 1) / ROW_GRID)); }
+__device__ __forceinline__ int64_t grid_row() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }  // the last may be past the rows
+
+// ---------------------------------------------------------------- joins over a wavefront and a workgroup
+// Lane i gets lane i ^ 1, i ^ 2, its mirror in 8 and in 16, then the other half of 32 and of 64: every lane ends with the
+// same value, added in the same order.
+template <int CTRL> __device__ __forceinline__ float dpp(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+template <typename OP> __device__ __forceinline__ float wave_join(float v, OP op)
+{
+    v = op(v, dpp<0xb1>(v));   // quad_perm 1 0 3 2
+    v = op(v, dpp<0x4e>(v));   // quad_perm 2 3 0 1
+    v = op(v, dpp<0x141>(v));  // row_half_mirror
+    v = op(v, dpp<0x140>(v));  // row_mirror
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+
+// The workgroup's sum (or maximum) of N values a thread, to every thread.  `lds` holds N * BLOCK / 64 floats; the barrier in
+// front lets it be used again at once.
+template <int BLOCK, int N, typename OP> __device__ __forceinline__ void block_join(float (&v)[N], float *lds, OP op)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_join(v[i], op);
+    if (BLOCK == 64) return;
+    constexpr int WAVES = BLOCK / 64;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) lds[i * WAVES + threadIdx.x / 64] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float r = lds[i * WAVES];
+        for (int w = 1; w < WAVES; ++w) r = op(r, lds[i * WAVES + w]);
+        v[i] = r;
+    }
+}
+
+}  // namespace omni

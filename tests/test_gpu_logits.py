@@ -1,0 +1,412 @@
+"""Log probabilities and the distillation loss on the GPU against 64 bits (oracle/network_end.py).  Bounds are counted in
+roundings of fp32 arithmetic (u = 2^-24): a row's sum is a chain of at most n / 64 terms a thread (n / 256 for n above 4096),
+rescaled at most once a chunk, and 14 joins -- chain(n) below -- and an exponent z costs 4 u |z| relative to its power; what is
+stored in bf16 is off by half a step (2^-8) more.  Indexes are equal."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import network_end as ne
+
+pytestmark = pytest.mark.gpu
+U, TINY = 2.0 ** -24, 1e-37
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1606_04487_amd import binding
+    assert torch.cuda.is_available()
+    return binding
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def chain(n):
+    return 2.0 * (n / 64 if n <= 4096 else n / 256) + 64
+
+
+def pitched(t, extra, pad=float("nan")):
+    rows, width = t.shape
+    full = torch.full((rows, width + extra), pad, dtype=t.dtype, device="cuda")
+    full[:, :width] = t
+    return full[:, :width]
+
+
+def untouched(t, extra, pad):
+    rows, width = t.shape
+    return extra == 0 or bool((t.as_strided((rows, extra), (width + extra, 1), t.storage_offset() + width) == pad).all())
+
+
+def near(got, ref, tol):
+    """Within tol where the reference is finite; the same infinities and NaN elsewhere.  A reference past fp32's largest value,
+    (2 - 2^-23) 2^127, is the infinity that it rounds to: a class of fp32's lowest value at temperature 1/4 has ln p = -1.4e39."""
+    ref = np.where(np.abs(ref) > np.finfo(np.float32).max, np.copysign(np.inf, ref), ref)
+    ok = np.isfinite(ref)
+    assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(got[~ok & ~np.isnan(ref)], ref[~ok & ~np.isnan(ref)])
+    assert np.all(np.abs(got[ok] - ref[ok]) <= np.broadcast_to(tol, ref.shape)[ok]), np.max((np.abs(got - ref) / np.broadcast_to(tol, ref.shape))[ok])
+
+
+def logits(rows, n, dtype, seed=1, sigma=2.5, masked=0.0):
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(rows, n, generator=g) * sigma).to(dtype)
+    if masked:
+        x[torch.rand(rows, n, generator=g) < masked] = -float("inf")
+    return x.cuda()
+
+
+def log_probabilities(x, temperature):
+    """(ln p, relative bound of p) of every element, in 64 bits."""
+    lp = np.array([ne.log_softmax_row(v, temperature) for v in x])
+    n = x.shape[1]
+    with np.errstate(invalid="ignore"):
+        return lp, U * (chain(n) + 8 * (np.where(np.isfinite(lp), np.abs(lp), 0.0) + np.log(n) + 1))
+
+
+def check_logprob(B, x, targets, top, temperature, extra=0, dlp=None, dh=None, entropy_too=True):
+    rows, n = x.shape
+    xg = pitched(x, extra)
+    lp, h, index, best, stats = B.logprob_forward(xg, targets, top, temperature)
+    xh = host(x)
+    tg = None if targets is None else targets.view(rows, -1).cpu().numpy()
+    rlp, rh, rindex, rbest = ne.logprob_forward(xh, tg, top, temperature)
+    full, rel = log_probabilities(xh, temperature)
+    worst = U * (chain(n) + 8 * (np.log(n) + 1))
+    if targets is not None:
+        near(host(lp).reshape(rows, -1), rlp, worst + 8 * U * np.abs(np.nan_to_num(rlp, neginf=0.0)))
+    near(host(h), rh, 2 * worst * (1 + np.log(n)))
+    if top:
+        assert np.array_equal(index.view(rows, top).cpu().numpy(), rindex)
+        near(host(best).reshape(rows, top), rbest, worst + 8 * U * np.abs(np.nan_to_num(rbest, neginf=0.0)))
+    if dlp is None and dh is None:
+        return
+    out = pitched(torch.zeros_like(x), extra, 7.0)
+    d = B.logprob_backward(xg, stats, targets, dlp, dh, h if dh is not None else None, temperature, out)
+    ref = ne.logprob_backward(xh, tg, None if dlp is None else host(dlp).reshape(rows, -1), None if dh is None else host(dh), temperature)
+    p, l = np.exp(full), np.where(np.isfinite(full), np.abs(full), 0.0)
+    factor = np.zeros_like(p) if dlp is None else np.abs(host(dlp).reshape(rows, -1)).sum(1)[:, None] + np.zeros_like(p)
+    if dh is not None:
+        factor = factor + np.abs(host(dh))[:, None] * (1 + l + rh[:, None])
+    listed = np.zeros_like(p)
+    if dlp is not None:
+        for r in range(rows):
+            for j, t in enumerate(tg[r]):
+                if 0 <= t < n:
+                    listed[r, t] += abs(float(host(dlp).reshape(rows, -1)[r, j]))
+    # a power below 2^-126 is zero, and |ln p| = 87 there: with a factor of 100 that is 1e-36, above TINY
+    tol = (2 * rel * factor * p + 2.0 ** -125 * factor + 1100 * U * listed) / temperature
+    near(host(d), ref, tol + half_step(x.dtype) * np.abs(ref) * 1.01 + TINY)
+    assert untouched(out, extra, 7.0)
+    inplace = xg.clone() if extra == 0 else xg
+    B.logprob_backward(inplace, stats, targets, dlp, dh, h if dh is not None else None, temperature, inplace)
+    assert torch.equal(inplace.view(torch.int16 if x.dtype == torch.bfloat16 else torch.int32),
+                       d.view(torch.int16 if x.dtype == torch.bfloat16 else torch.int32))
+
+
+# lengths around the chunks' and workgroups' edges, to long ones
+LENGTHS = [1, 2, 3, 7, 8, 9, 15, 17, 63, 65, 255, 257, 511, 1000, 1025, 2049, 4099, 5003, 8193, 16385, 33001, 70001, 131072]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", LENGTHS)
+def test_logprob_lengths(B, n, dtype):
+    for rows, extra, temperature, top in ((3, 0, 1.0, 5), (2, 1, 0.7, 64)):
+        x = logits(rows, n, dtype, seed=n)
+        g = torch.Generator().manual_seed(n)
+        targets = torch.randint(0, n, (rows,), generator=g).cuda()
+        check_logprob(B, x, targets, top, temperature, extra, torch.randn(rows, generator=g).cuda(), torch.randn(rows, generator=g).cuda())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n,top", [(700, 40, 3), (520, 9001, 20), (1030, 2600, 0), (257, 1000, 5)])
+def test_logprob_many_rows(B, rows, n, top, dtype):
+    x = logits(rows, n, dtype, masked=0.1)
+    g = torch.Generator().manual_seed(5)
+    targets = torch.randint(0, n, (rows,), generator=g).cuda()
+    check_logprob(B, x, targets, top, 1.3, 0, torch.randn(rows, generator=g).cuda())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,given", [(5, 1024), (1000, 3), (9001, 17), (300, 256)])
+def test_logprob_several_targets(B, n, given, dtype):
+    rows, g = 4, torch.Generator().manual_seed(3)
+    targets = torch.randint(-n // 4, n, (rows, given), generator=g)      # some left out, many named twice
+    targets[1] = -1
+    targets[2, :given // 2] = n - 1
+    check_logprob(B, logits(rows, n, dtype), targets.cuda(), 0, 2.0, 3, torch.randn(rows, given, generator=g).cuda(), torch.randn(rows, generator=g).cuda())
+
+
+def test_logprob_entropy_or_targets_alone(B):
+    x = logits(9, 777, torch.float32)
+    check_logprob(B, x, None, 0, 1.0, 0, None, torch.randn(9).cuda())
+    t = torch.randint(0, 777, (9,)).cuda()
+    a = B.logprob_forward(x, t, want_entropy=False, want_stats=False)
+    b = B.logprob_forward(x, t, 7)
+    assert a[1] is None and a[2] is None and a[4] is None and torch.equal(a[0], b[0])
+
+
+def out_of_the_ordinary(n, dtype):
+    lo = torch.finfo(dtype).min
+    x = logits(12, n, dtype, seed=n)
+    inf = float("inf")
+    x[0] = -inf                                  # nothing possible
+    x[1] = -inf
+    x[1, n // 2] = 3.0                           # one class possible
+    x[2] = lo                                    # the type's lowest value everywhere: uniform
+    x[3, : n - n // 3] = lo                      # ... as a mask
+    x[4] = 0.0                                   # all equal
+    x[5, n // 3] = float("nan")
+    x[6, n - 1] = inf
+    x[7, 0] = float("nan")
+    x[7, 1:] = -inf
+    x[8] = torch.arange(n).to(dtype)             # ascending
+    x[9] = torch.arange(n).flip(0).to(dtype)
+    x[10, : n // 2] = 1e4                        # many equal largest
+    x[11, ::2] = -0.0
+    x[11, 1::2] = 0.0                            # signed zeros are equal
+    return x
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [6, 100, 1001, 9001, 40000])
+def test_logprob_out_of_the_ordinary(B, n, dtype):
+    x = out_of_the_ordinary(n, dtype)
+    for temperature in (1.0, 0.25):
+        targets = torch.tensor([[0, n // 2, -1]] * 12).cuda()
+        dlp, dh = torch.randn(12, 3).cuda(), torch.randn(12).cuda()
+        check_logprob(B, x, targets, min(n, 20), temperature, 0, dlp, dh)
+    x = logits(3, n, dtype)
+    targets = torch.tensor([[0], [n], [2 ** 40]]).cuda()                 # past the classes: NaN, and no access there
+    check_logprob(B, x, targets, 1, 1.0, 0, torch.ones(3, 1).cuda())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows", [2, 600])
+def test_top_alternatives_oddly_placed(B, rows, dtype):
+    # the largest values all in the chunks of one thread, for workgroups of 64, 256 and 1024 threads; more equal values than the
+    # collection has room for, at the end and everywhere
+    n = 40000
+    for period in (64, 256, 1024):
+        x = logits(rows, n, dtype, sigma=0.5)
+        v = 16 // x.element_size()
+        at = (torch.arange(n) // v) % period == 3
+        x[:, at.cuda()] = 50.0 + torch.randint(0, 40, (int(at.sum()),)).to(dtype).cuda()
+        check_logprob(B, x, None, 64, 1.0)
+    x = logits(rows, n, dtype, sigma=0.5)
+    x[0, 20000:] = 30.0
+    x[1, 39000:] = 30.0
+    x[1, 38990] = 31.0
+    check_logprob(B, x, None, 33, 1.0)
+
+
+def test_logprob_many_rows_and_far_offsets(B):
+    rows = (1 << 20) + 5
+    x = torch.randn(rows, 5, device="cuda")
+    t = torch.randint(0, 5, (rows,), device="cuda")
+    lp, h, index, best, stats = B.logprob_forward(x, t, 2)
+    d = B.logprob_backward(x, stats, t, torch.ones(rows, device="cuda"))
+    full = torch.log_softmax(x.double(), 1)
+    assert float((lp - full.gather(1, t[:, None])[:, 0]).abs().max()) < 200 * U * 10
+    assert torch.equal(index, x.topk(2, dim=1).indices)
+    ref = -full.exp()
+    ref.scatter_add_(1, t[:, None], torch.ones(rows, 1, dtype=torch.float64, device="cuda"))
+    assert float((d - ref).abs().max()) < 200 * U * 10
+    ld = (1 << 30) + 8
+    whole = torch.empty(2 * ld + 5000, dtype=torch.bfloat16, device="cuda")
+    far, close = whole.as_strided((3, 5000), (ld, 1)), logits(3, 5000, torch.bfloat16)
+    far.copy_(close)
+    t = torch.tensor([0, 4999, 7], device="cuda")
+    a, b = B.logprob_forward(close, t, 9), B.logprob_forward(far, t, 9)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    one = torch.ones(3, device="cuda")
+    want = B.logprob_backward(close, a[4], t, one)
+    assert torch.equal(B.logprob_backward(far, a[4], t, one, dlogits=far), want)
+    far.copy_(close)
+    want = B.distill_forward_backward(close, labels=t, alpha=0.0)
+    got = B.distill_forward_backward(far, labels=t, alpha=0.0, dlogits=far)
+    assert torch.equal(got[0], want[0]) and torch.equal(far, want[1])
+    del whole, far
+    torch.cuda.empty_cache()
+
+
+# ---------------------------------------------------------------- distillation
+def teacher(rows, n, kept, seed, ragged=True):
+    g = torch.Generator().manual_seed(seed)
+    index = torch.stack([torch.randperm(n, generator=g)[:kept] if kept <= n else torch.randint(0, n, (kept,), generator=g) for _ in range(rows)])
+    values = torch.randn(rows, kept, generator=g) * 3
+    if ragged and rows > 2 and kept > 1:
+        index[0, kept // 2:] = -1
+        values[1, 0] = -float("inf")
+        index[2] = -1                            # a row without entries
+        index[rows - 1, kept - 1] = index[rows - 1, 0]                   # the same class twice
+    labels = torch.randint(0, n, (rows,), generator=g)
+    labels[rows // 2] = -1
+    if rows > 1:
+        labels[rows - 1] = index[rows - 1, 0]
+    return index.cuda(), values.cuda(), labels.cuda(), torch.rand(rows, generator=g).cuda() + 0.5
+
+
+def check_distill(B, x, index, values, labels, w, temperature, alpha, extra=0):
+    rows, n = x.shape
+    xg, out = pitched(x, extra), pitched(torch.zeros_like(x), extra, 7.0)
+    args = (index, values, labels, temperature, alpha)
+    loss, stats = B.distill_forward(xg, *args)
+    d = B.distill_backward(xg, *args, stats=stats, dloss=w, scale=0.5, dlogits=out)
+    xh, soft = host(x), index is not None and alpha > 0
+    ih, vh = (index.cpu().numpy(), host(values)) if soft else (None, None)
+    lh = None if labels is None else labels.cpu().numpy()
+    rloss, rd = ne.distill(xh, ih, vh, lh, temperature, alpha, 0.5 * host(w))
+    lp, rel = log_probabilities(xh, temperature)
+    lp1, rel1 = log_probabilities(xh, 1.0)
+    mag, tol = np.zeros(rows), TINY + np.zeros((rows, n))
+    ws = 0.5 * host(w)
+    for r in range(rows):
+        if soft:
+            there = (ih[r] >= 0) & (ih[r] < n) & np.isfinite(vh[r])
+            at, t = ih[r][there], vh[r][there]
+            if at.size:
+                lnq = ne.log_softmax_row(t, temperature)
+                q, l = np.exp(lnq), np.nan_to_num(np.abs(lp[r, at]), nan=0.0, posinf=0.0)
+                mag[r] += alpha * temperature ** 2 * (q * (1 + np.abs(lnq) + l) * (chain(n) + 300 + 8 * (np.abs(lnq) + l + np.log(n) + 1))).sum()
+                tol[r] += ws[r] * alpha * temperature * np.nan_to_num(np.exp(lp[r]) * rel[r], nan=0.0)
+                np.add.at(tol[r], at, ws[r] * alpha * temperature * q * U * (600 + 8 * np.abs(lnq)))
+        if lh is not None and alpha < 1 and 0 <= lh[r] < n:
+            l = np.nan_to_num(abs(lp1[r, lh[r]]), nan=0.0, posinf=0.0)
+            mag[r] += (1 - alpha) * (chain(n) + 8 * (l + np.log(n) + 1)) * 1.0
+            tol[r] += ws[r] * (1 - alpha) * np.nan_to_num(np.exp(lp1[r]) * rel1[r], nan=0.0)
+            tol[r, lh[r]] += ws[r] * (1 - alpha) * 8 * U
+    near(host(loss), rloss, U * mag + 4 * U * np.abs(np.nan_to_num(rloss, posinf=0.0)))
+    bound = 1.5 * tol + 8 * U * np.abs(np.nan_to_num(rd)) + half_step(x.dtype) * np.abs(np.nan_to_num(rd)) * 1.01
+    near(host(d), rd, bound)
+    assert untouched(out, extra, 7.0)
+    both = pitched(torch.zeros_like(x), extra, 7.0)
+    loss2, d2 = B.distill_forward_backward(xg, *args, dloss=w, scale=0.5, dlogits=both)
+    near(host(loss2), rloss, U * mag + 4 * U * np.abs(np.nan_to_num(rloss, posinf=0.0)))
+    near(host(d2), rd, bound)
+    assert untouched(both, extra, 7.0)
+    for again in range(2):                       # bit-identical, also over the logits themselves
+        to = xg.clone() if extra == 0 else pitched(x, extra)
+        loss3, _ = B.distill_forward_backward(to, *args, dloss=w, scale=0.5, dlogits=to)
+        assert torch.equal(loss3.view(torch.int32), loss2.view(torch.int32)) and np.array_equal(host(to), host(d2), equal_nan=True)
+    B.distill_backward(xg, *args, stats=stats, dloss=w, scale=0.5, dlogits=xg)
+    assert np.array_equal(host(xg), host(d), equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", LENGTHS)
+def test_distill_lengths(B, n, dtype):
+    for rows, kept, temperature, alpha, extra in ((4, 5, 2.0, 0.6, 0), (3, 33, 1.0, 1.0, 1)):
+        check_distill(B, logits(rows, n, dtype, seed=n), *teacher(rows, n, kept, n), temperature, alpha, extra)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n,kept,temperature,alpha", [(600, 50, 256, 3.0, 0.5), (515, 9001, 8, 1.0, 0.4), (300, 1000, 10, 4.0, 0.7), (1100, 2500, 1, 0.5, 1.0)])
+def test_distill_many_rows(B, rows, n, kept, temperature, alpha, dtype):
+    check_distill(B, logits(rows, n, dtype), *teacher(rows, n, kept, 3), temperature, alpha)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_cross_entropy_alone_and_each_part_alone(B, dtype):
+    x = logits(37, 1000, dtype)
+    index, values, labels, w = teacher(37, 1000, 6, 1)
+    check_distill(B, x, None, None, labels, w, 1.0, 0.0)
+    check_distill(B, x, None, None, labels, w, 5.0, 0.0)
+    check_distill(B, x, None, None, labels, w, 5.0, 0.3)
+    check_distill(B, x, index, values, None, w, 2.0, 0.3)
+    check_distill(B, x, index, values, labels, w, 2.0, 1.0)
+    check_distill(B, x, index, values, labels, w, 2.0, 0.0)
+    loss, d = B.distill_forward_backward(x, labels=labels, alpha=0.0)      # no weights: ones
+    one, d1 = B.distill_forward_backward(x, labels=labels, alpha=0.0, dloss=torch.ones(37, device="cuda"))
+    assert torch.equal(loss, one) and torch.equal(d, d1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [6, 1001, 9001, 40000])
+@pytest.mark.parametrize("temperature,alpha", [(2.0, 0.5), (0.25, 1.0), (1.0, 0.0)])
+def test_distill_out_of_the_ordinary(B, n, temperature, alpha, dtype):
+    x = out_of_the_ordinary(n, dtype)
+    index = torch.tensor([[0, n // 2, n - 1, 1]] * 12)
+    values = torch.tensor([[0.5, -1.0, 2.0, -float("inf")]] * 12)
+    labels = torch.arange(12) % n
+    labels[4] = -100
+    check_distill(B, x, index.cuda(), values.cuda(), labels.cuda(), torch.ones(12).cuda(), temperature, alpha)
+    # entries and labels past the classes, and entries that are no numbers: NaN, and no access there
+    x = logits(5, n, dtype)
+    index, values, labels = torch.zeros((5, 2), dtype=torch.int64), torch.zeros(5, 2), torch.zeros(5, dtype=torch.int64)
+    index[0, 1], index[1, 0], values[2, 1], values[3, 0], labels[4] = n, 2 ** 40, float("nan"), float("inf"), n
+    check_distill(B, x, index.cuda(), values.cuda(), labels.cuda(), torch.ones(5).cuda(), temperature, alpha)
+
+
+def test_gradients_by_differences(B):
+    # fp32 losses of a few rows against their gradients: central differences of width h = 2^-6 are off by h^2 / 6 times the third
+    # derivative (of a log-sum-exp at most 0.1, of an entropy at most 8) plus the rounding of two losses of at most 10, over h
+    rows, n, h = 3, 21, 2.0 ** -6
+    x = logits(rows, n, torch.float32, sigma=1.0)
+    index, values, labels, w = teacher(rows, n, 4, 9, ragged=False)
+    _, d = B.distill_forward_backward(x, index, values, labels, 2.0, 0.5, dloss=w)
+    lp0, h0, _, _, stats = B.logprob_forward(x, labels.clamp(min=0))
+    e = B.logprob_backward(x, stats, labels.clamp(min=0), w, w, h0)
+    for i in range(n):
+        up, down = x.clone(), x.clone()
+        up[:, i] += h
+        down[:, i] -= h
+        step = (up[:, i] - down[:, i]).double()
+        fd = (B.distill_forward(up, index, values, labels, 2.0, 0.5)[0] - B.distill_forward(down, index, values, labels, 2.0, 0.5)[0]).double() * w / step
+        assert float((fd - d[:, i]).abs().max()) < 1.5 * h * h + 64 * U * 10 * 1.5 / h
+        a, b = B.logprob_forward(up, labels.clamp(min=0)), B.logprob_forward(down, labels.clamp(min=0))
+        fd = ((a[0] - b[0]).double() + (a[1] - b[1]).double()) * w / step
+        assert float((fd - e[:, i]).abs().max()) < 1.5 * 8 * h * h + 64 * U * 20 * 1.5 / h
+
+
+def test_together_on_other_streams_and_in_a_replayed_graph(B):
+    """The teacher's top alternatives are the student's entries: one after the other, on a side stream, and as one graph."""
+    rows, n, k = 300, 5001, 12
+    student, big = logits(rows, n, torch.bfloat16, seed=1), logits(rows, n, torch.bfloat16, seed=2)
+    labels = torch.randint(0, n, (rows,)).cuda()
+    w = torch.rand(rows).cuda()
+    index, best = torch.empty((rows, k), dtype=torch.int64, device="cuda"), torch.empty((rows, k), device="cuda")
+    loss, out = torch.empty(rows, device="cuda"), torch.empty_like(student)
+    lp, h, st = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty((rows, 2), device="cuda")
+    ws = [torch.empty(max(16, b), dtype=torch.uint8, device="cuda") for b in
+          (B.logprob_workspace_bytes(rows, n, k, torch.bfloat16), B.distill_workspace_bytes(rows, n, torch.bfloat16))]
+
+    def together():
+        B.logprob_forward(big, labels, k, logprob=lp, entropy=h, top_index=index, top_logprob=best, stats=st, workspace=ws[0])
+        B.distill_forward_backward(student, index, best, labels, 2.0, 0.5, dloss=w, loss=loss, dlogits=out, workspace=ws[1])
+        B.logprob_backward(student, st, labels, w, dlogits=big)          # (with the teacher's sums: only its repetition is looked at)
+    outs = (index, best, loss, out, lp, h, st, big)
+    side = torch.cuda.Stream()
+    keep = big.clone()
+    together()
+    want = [t.clone() for t in outs]
+    rl, rd = ne.distill(host(student), index.cpu().numpy(), host(best), labels.cpu().numpy(), 2.0, 0.5, host(w))
+    assert np.max(np.abs(host(loss) - rl)) <= U * 4 * (chain(n) + 400) * 25
+    assert np.all(np.abs(host(out) - rd) <= half_step(torch.bfloat16) * np.abs(rd) * 1.01 + U * 2 * (chain(n) + 600 + 400))
+    big.copy_(keep)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        together()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, outs))
+    graph = torch.cuda.CUDAGraph()
+    big.copy_(keep)
+    with torch.cuda.graph(graph):
+        together()
+    for i in range(3):
+        keep.mul_(1.5)
+        student.add_(0.125 * (i + 1))
+        big.copy_(keep)
+        together()
+        want = [t.clone() for t in outs]
+        big.copy_(keep)
+        for t in (index, best, loss, out, lp, h, st):
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outs))
