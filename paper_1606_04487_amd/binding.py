@@ -36,8 +36,8 @@ SYMBOLS = [
     "omni_conv_dy_rows_layout", "omni_relu_backward_rows", "omni_maxpool_backward_rows", "omni_conv_backward_weights_rows",
     "omni_conv_backward_data_rows", "omni_conv_backward_data_relu_rows_sums", "omni_conv_backward_data_relu_rows",
     "omni_lrn_forward", "omni_lrn_backward", "omni_dropout_forward", "omni_dropout_backward",
-    "omni_layer_norm_forward", "omni_layer_norm_workspace_bytes", "omni_layer_norm_backward", "omni_logprob_workspace_bytes",
-    "omni_logprob_forward", "omni_logprob_backward", "omni_distill_workspace_bytes", "omni_distill_forward", "omni_distill_backward",
+    "omni_layer_norm_forward", "omni_layer_norm_workspace_bytes", "omni_layer_norm_backward", 
+    "omni_logprob_forward", "omni_logprob_backward", "omni_distill_forward", "omni_distill_backward",
     "omni_distill_forward_backward", "omni_status_string", "omni_version", "omni_tuning_set",
     "omni_profile_enable", "omni_profile_select", "omni_profile_select_mask", "omni_profile_kernel_count", "omni_profile_kernel_name", "omni_profile_summary",
 ]
@@ -105,13 +105,11 @@ _lib.omni_dropout_backward.argtypes = [_i32, _i64, _f, _u64, _u64, _vp, _vp, _vp
 _lib.omni_layer_norm_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _f, _vp, _i64, _vp, _vp, _vp]
 _lib.omni_layer_norm_workspace_bytes.argtypes = [_i32, _i64, _i64, ctypes.POINTER(_sz)]
 _lib.omni_layer_norm_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _sz, _vp]
-_lib.omni_logprob_workspace_bytes.argtypes = [_i32, _i64, _i64, _i32, ctypes.POINTER(_sz)]
-_lib.omni_logprob_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _f, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.omni_logprob_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _f, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp]
 _lib.omni_logprob_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _f, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _i64, _vp]
-_lib.omni_distill_workspace_bytes.argtypes = [_i32, _i64, _i64, ctypes.POINTER(_sz)]
-_lib.omni_distill_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _vp, _vp, _sz, _vp]
+_lib.omni_distill_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _vp, _vp]
 _lib.omni_distill_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _vp, _f, _vp, _i64, _vp]
-_lib.omni_distill_forward_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _f, _vp, _vp, _i64, _vp, _sz, _vp]
+_lib.omni_distill_forward_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _f, _vp, _vp, _i64, _vp]
 
 _lib.omni_profile_enable.argtypes = [ctypes.c_int]
 _lib.omni_profile_select_mask.argtypes = [ctypes.c_uint64]
@@ -655,13 +653,6 @@ def layer_norm_backward(x, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbe
     return dx, dgamma, dbeta
 
 
-def logprob_workspace_bytes(rows: int, classes: int, top: int = 0, dtype: torch.dtype = torch.float32) -> int:
-    """omni_logprob_workspace_bytes: scratch of logprob_forward (0: none)."""
-    b = _sz()
-    _check(_lib.omni_logprob_workspace_bytes(dtype_code(dtype), rows, classes, top, ctypes.byref(b)))
-    return b.value
-
-
 def _given(targets, rows: int) -> int:
     if targets is None:
         return 0
@@ -671,7 +662,7 @@ def _given(targets, rows: int) -> int:
 
 
 def logprob_forward(logits, targets=None, top: int = 0, temperature: float = 1.0, logprob=None, entropy=None, top_index=None,
-                    top_logprob=None, stats=None, want_entropy: bool = True, want_stats: bool = True, workspace=None):
+                    top_logprob=None, stats=None, want_entropy: bool = True, want_stats: bool = True):
     """omni_logprob_forward over logits [..., classes]; returns (logprob, entropy, top_index, top_logprob, stats).  targets:
     int64, any number of classes a row; logprob has targets' shape, entropy one value a row, top_index (int64) and top_logprob
     `top` a row; stats is what logprob_backward needs."""
@@ -687,12 +678,10 @@ def logprob_forward(logits, targets=None, top: int = 0, temperature: float = 1.0
         top_logprob = torch.empty(lead + (top,), dtype=f32, device=dev) if top_logprob is None else top_logprob
     if stats is None and want_stats:
         stats = torch.empty(lead + (2,), dtype=f32, device=dev)
-    need = logprob_workspace_bytes(rows, classes, top, logits.dtype) if workspace is None else 0
-    pw, nw, keep = _scratch(need, workspace, dev)
     _check(_lib.omni_logprob_forward(code, rows, classes, p, ld, temperature, _vector(targets, rows * given, i64, "targets"), given,
                                      _vector(logprob, rows * given, f32, "logprob"), _vector(entropy, rows, f32, "entropy"), top,
                                      _vector(top_index, rows * top, i64, "top_index"), _vector(top_logprob, rows * top, f32, "top_logprob"),
-                                     _vector(stats, 2 * rows, f32, "stats"), pw, nw, _stream()))
+                                     _vector(stats, 2 * rows, f32, "stats"), _stream()))
     return logprob, entropy, top_index, top_logprob, stats
 
 
@@ -711,13 +700,6 @@ def logprob_backward(logits, stats, targets=None, dlogprob=None, dentropy=None, 
     return dlogits
 
 
-def distill_workspace_bytes(rows: int, classes: int, dtype: torch.dtype = torch.float32) -> int:
-    """omni_distill_workspace_bytes: scratch of distill_forward and distill_forward_backward (0: none)."""
-    b = _sz()
-    _check(_lib.omni_distill_workspace_bytes(dtype_code(dtype), rows, classes, ctypes.byref(b)))
-    return b.value
-
-
 def _teacher(index, values, labels, rows: int):
     """(index pointer, logits pointer, entries a row, labels pointer)"""
     if (index is None) != (values is None):
@@ -732,7 +714,7 @@ def _teacher(index, values, labels, rows: int):
 
 
 def distill_forward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0, loss=None,
-                    stats=None, want_stats: bool = True, workspace=None):
+                    stats=None, want_stats: bool = True):
     """omni_distill_forward over logits [..., classes]; returns (loss, stats): the loss of every row, and what distill_backward
     needs.  Without teacher entries (and alpha = 0) it is the labels' cross entropy."""
     p, rows, classes, ld = _matrix(logits, "logits")
@@ -741,10 +723,8 @@ def distill_forward(logits, teacher_index=None, teacher_logits=None, labels=None
     loss = torch.empty(logits.shape[:-1], dtype=f32, device=dev) if loss is None else loss
     if stats is None and want_stats:
         stats = torch.empty(tuple(logits.shape[:-1]) + (4,), dtype=f32, device=dev)
-    need = distill_workspace_bytes(rows, classes, logits.dtype) if workspace is None else 0
-    pw, nw, keep = _scratch(need, workspace, dev)
     _check(_lib.omni_distill_forward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                     _vector(loss, rows, f32, "loss"), _vector(stats, 4 * rows, f32, "stats"), pw, nw, _stream()))
+                                     _vector(loss, rows, f32, "loss"), _vector(stats, 4 * rows, f32, "stats"), _stream()))
     return loss, stats
 
 
@@ -763,7 +743,7 @@ def distill_backward(logits, teacher_index=None, teacher_logits=None, labels=Non
 
 
 def distill_forward_backward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0,
-                             dloss=None, scale: float = 1.0, loss=None, dlogits=None, workspace=None):
+                             dloss=None, scale: float = 1.0, loss=None, dlogits=None):
     """omni_distill_forward_backward: distill_forward and distill_backward in one call; returns (loss, dlogits)."""
     p, rows, classes, ld = _matrix(logits, "logits")
     f32, dev = torch.float32, logits.device
@@ -772,10 +752,8 @@ def distill_forward_backward(logits, teacher_index=None, teacher_logits=None, la
     if dlogits is None:
         dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
     po, ldo = _like(dlogits, rows, classes, logits.dtype, "dlogits")
-    need = distill_workspace_bytes(rows, classes, logits.dtype) if workspace is None else 0
-    pw, nw, keep = _scratch(need, workspace, dev)
     _check(_lib.omni_distill_forward_backward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                              _vector(dloss, rows, f32, "dloss"), scale, _vector(loss, rows, f32, "loss"), po, ldo, pw, nw,
+                                              _vector(dloss, rows, f32, "dloss"), scale, _vector(loss, rows, f32, "loss"), po, ldo,
                                               _stream()))
     return loss, dlogits
 

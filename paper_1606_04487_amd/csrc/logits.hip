@@ -6,6 +6,10 @@
 // has no probability and a row of nothing else none at all (m = -inf, s = 0).  A NaN or +inf makes the row's results NaN.
 #include "row_ops.h"
 
+// Products and sums are fused where fmaf says so and nowhere else: a row's sums are then the same bits in every variant of a
+// kernel, whatever else it computes.
+#pragma clang fp contract(off)
+
 namespace omni {
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
@@ -35,92 +39,171 @@ template <typename T> struct RowSplit {
     __device__ __forceinline__ int first(int c) const { return c * CHUNK<T> - shift; }
 };
 
-template <typename T> __device__ __forceinline__ void aligned_chunk(const T *row, int at, float (&v)[CHUNK<T>])
+// A chunk of the row as it lies in memory.  NT: it is used once, so it goes past the caches (rows read straight through:
+// 6.9 TB/s, 6.2 through the caches; 2^29 bytes in rows of 64 to 256 KB).
+template <typename T, bool NT> __device__ __forceinline__ uint4 raw_chunk(const T *row, int at)
 {
-    const uint4 b = *reinterpret_cast<const uint4 *>(row + at);
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    const words *p = reinterpret_cast<const words *>(row + at);
+    const words w = NT ? __builtin_nontemporal_load(p) : *p;
+    return make_uint4(w.x, w.y, w.z, w.w);
+}
+template <typename T> __device__ __forceinline__ void unpack(const uint4 &b, float *v)
+{
     const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-    unpack(w, v);
+    float u[CHUNK<T>];
+    unpack(w, u);
+#pragma unroll
+    for (int j = 0; j < CHUNK<T>; ++j) v[j] = u[j];
 }
 
 // ------------------------------------------------------------------------------------------------ running sums
-// s = sum e^z, t = sum z e^z (in powers of two: z is scaled by log2 e / T) relative to m.
-struct Sums { float m, s, t; };
+// Powers of two throughout: e^z = 2^(c (x - m)), c = log2 e / T.  s = sum of them, and in t
+enum Also {
+    NOTHING,
+    Z_TIMES,   // sum z e^z: the entropy's
+    AT_ONE,    // the sum at T = 1, by a second exponential
+    SQUARED,   // ... which at T = 2 is the first one's square
+    SQUARED2,  // ... and at T = 4 its fourth power
+};
+// All are relative to the power h = m c as fp32 rounds it, so that an exponent is one fused product and sum, x c - h; finish()
+// takes the rounding, m c - h < 2^-4, out of them.  Where m c is so large that its rounding is a power of its own (masks of the
+// type's lowest value, m of +inf) they are relative to m c itself and the difference x - m is taken first.
+struct Sums {
+    float m, h, s, t;
+    __device__ __forceinline__ float m0() const { return m == -INFINITY ? 0.f : m; }
+    __device__ __forceinline__ bool far() const { return !(fabsf(h) < 1048576.f); }
+    __device__ __forceinline__ float rounding(float c) const { return far() ? 0.f : fmaf(m0(), c, -h); }  // exact
+};
 
-// SUMS: 1 s, 2 s and t, -1 s and, in t's place, the sum at T = 1
-template <int SUMS> __device__ __forceinline__ void rescale(Sums &a, float m, float c, float c1)
+template <int ALSO> __device__ __forceinline__ float at_one(float e, float d) { return ALSO == SQUARED ? e * e : ALSO == SQUARED2 ? (e * e) * (e * e) : exp2_fast(d * LOG2E); }
+
+template <int ALSO> __device__ __forceinline__ void rescale(Sums &a, float m, float c)
 {
     if (a.m == m) return;
-    if (a.m == -INFINITY) {  // nothing so far (or NaN, which stays)
-        a.m = m;
-        return;
+    const Sums b = {m, m * c, a.s, a.t};
+    if (a.m > -INFINITY) {  // (else there is nothing so far, or NaN, which stays)
+        const float z = fmaf(a.m - m, c, b.rounding(c) - a.rounding(c)), f = exp2_fast(z);
+        if (ALSO == Z_TIMES) a.t = f > 0.f ? (a.t + z * a.s) * f : 0.f;
+        if (ALSO >= AT_ONE) a.t *= at_one<ALSO>(f, a.m - m);
+        a.s *= f;
     }
-    const float d = (a.m - m) * c, f = exp2_fast(d);
-    if (SUMS == 2) a.t = f > 0.f ? (a.t + d * a.s) * f : 0.f;
-    if (SUMS == -1) a.t *= exp2_fast((a.m - m) * c1);
-    a.s *= f;
     a.m = m;
+    a.h = b.h;
 }
 
-template <int SUMS, int N> __device__ __forceinline__ void absorb(Sums &a, const float (&x)[N], float c, float c1)
+// To sums relative to m itself.
+template <int ALSO> __device__ __forceinline__ void finish(Sums &a, float c)
+{
+    const float z = -a.rounding(c), f = exp2_fast(z);
+    if (ALSO == Z_TIMES) a.t = (a.t + z * a.s) * f;
+    if (ALSO > AT_ONE) a.t *= at_one<ALSO>(f, 0.f);
+    a.s *= f;
+}
+
+template <int ALSO, int N> __device__ __forceinline__ void absorb(Sums &a, const float (&x)[N], float c)
 {
     float g = x[0];
 #pragma unroll
     for (int j = 1; j < N; ++j) g = fmaxf(g, x[j]);
-    if (g > a.m) rescale<SUMS>(a, g, c, c1);
-    const float m = a.m == -INFINITY ? 0.f : a.m;
+    if (g > a.m) rescale<ALSO>(a, g, c);
+    if (__any(a.far())) {  // the difference first
+        const float m = a.m0(), r = a.rounding(c);
+        for (int j = 0; j < N; ++j) {
+            const float d = x[j] - m, z = fmaf(d, c, r), e = exp2_fast(z);
+            a.s += e;
+            if (ALSO == Z_TIMES) a.t += fmaxf(z, Z_LEAST) * e;
+            if (ALSO >= AT_ONE) a.t += at_one<ALSO>(e, d);
+        }
+        return;
+    }
+    // two chains of sums
+    float s1 = 0.f, t1 = 0.f;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        const float d = x[j] - m, z = d * c, e = exp2_fast(z);
-        a.s += e;
-        if (SUMS == 2) a.t += fmaxf(z, Z_LEAST) * e;
-        if (SUMS == -1) a.t += exp2_fast(d * c1);
+        const float z = fmaf(x[j], c, -a.h), e = exp2_fast(z);
+        (j % 2 ? s1 : a.s) += e;
+        float &t = j % 2 ? t1 : a.t;
+        if (ALSO == Z_TIMES) t = fmaf(fmaxf(z, Z_LEAST), e, t);
+        if (ALSO == AT_ONE) t += exp2_fast((x[j] - a.m0()) * LOG2E);
+        if (ALSO == SQUARED) t = fmaf(e, e, t);
+        if (ALSO == SQUARED2) t = fmaf(e * e, e * e, t);
     }
+    a.s += s1;
+    a.t += t1;
 }
 
-template <int SUMS, int BLOCK> __device__ __forceinline__ void join(Sums &a, float c, float c1, float *lds)
+template <int ALSO, int BLOCK> __device__ __forceinline__ void join(Sums &a, float c, float *lds)
 {
     float m[1] = {a.m}, v[2];
     block_join<BLOCK>(m, lds, Max());
-    rescale<SUMS>(a, m[0], c, c1);
+    rescale<ALSO>(a, m[0], c);
     v[0] = a.s, v[1] = a.t;
     block_join<BLOCK>(v, lds, Add());
     a.s = v[0], a.t = v[1];
+    finish<ALSO>(a, c);
 }
 
-constexpr int UNROLL = 4;  // chunks a thread loads before it uses the first
+constexpr int PAIR = 2;  // chunks whose sums are taken together
 
-// The sums over a row; the thread's own maximum (for the top alternatives) goes to *own.
-template <typename T, int BLOCK, int SUMS> __device__ __forceinline__ Sums row_sums(const T *row, int n, const RowSplit<T> &sp, float c, float c1, float *own, float *lds)
+// The sums over a row; the thread's own maximum (for the top alternatives) goes to *own.  KEPT chunks a thread, the first ones,
+// are loaded at once and stay in `kept`; the others follow in batches of 4, the next batch in flight while one is summed.
+template <typename T, int BLOCK, int ALSO, bool NT, int KEPT>
+__device__ __forceinline__ Sums row_sums(const T *row, int n, const RowSplit<T> &sp, float c, float *own, float *lds, uint4 (&kept)[KEPT > 0 ? KEPT : 1])
 {
-    constexpr int V = CHUNK<T>;
-    Sums a = {-INFINITY, 0.f, 0.f};
-    const int tid = threadIdx.x;
-    int at = sp.lo;
-    for (; at + UNROLL * BLOCK <= sp.hi; at += UNROLL * BLOCK) {
-        float x[UNROLL][V];
+    constexpr int V = CHUNK<T>, BATCH = 4;
+    static_assert(KEPT % PAIR == 0 && BATCH % PAIR == 0, "whole pairs");
+    Sums a = {-INFINITY, 0.f, 0.f, 0.f};  // (no maximum yet: h = 0)
+    const int tid = threadIdx.x, last = sp.hi - 1;
+    auto take = [&](const uint4 *b, int at, bool whole) {  // two chunks; those past the last one, which repeat it, count as -inf
+        float x[PAIR * V];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) aligned_chunk(row, sp.first(at + u * BLOCK + tid), x[u]);
+        for (int u = 0; u < PAIR; ++u) {
+            unpack<T>(b[u], x + u * V);
+            if (!whole)
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) absorb<SUMS>(a, x[u], c, c1);
-    }
-    if (at < sp.hi) {  // the last chunks: loads past them repeat the last one and count as -inf
-        float x[UNROLL][V];
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int k = at + u * BLOCK + tid;
-            aligned_chunk(row, sp.first(k < sp.hi ? k : sp.hi - 1), x[u]);
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[u][j] = k < sp.hi ? x[u][j] : -INFINITY;
+                for (int j = 0; j < V; ++j) x[u * V + j] = at + u * BLOCK <= last ? x[u * V + j] : -INFINITY;
         }
+        absorb<ALSO>(a, x, c);
+    };
+    auto load = [&](uint4 &b, int at) { b = raw_chunk<T, NT>(row, sp.first(at < last ? at : last)); };
+    int at = sp.lo + tid;
+    if (KEPT > 0 && sp.lo < sp.hi) {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) absorb<SUMS>(a, x[u], c, c1);
+        for (int u = 0; u < KEPT; ++u) load(kept[u], at + u * BLOCK);
+#pragma unroll
+        for (int u = 0; u < KEPT; u += PAIR) {
+            const int first = sp.lo + u * BLOCK;
+            if (first < sp.hi) take(kept + u, at + u * BLOCK, first + PAIR * BLOCK <= sp.hi);
+        }
+    }
+    at += KEPT * BLOCK;
+    int first = sp.lo + KEPT * BLOCK;
+    if (first < sp.hi) {
+        uint4 b[BATCH], next[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) load(b[u], at + u * BLOCK);
+        for (;;) {
+            const bool more = first + BATCH * BLOCK < sp.hi;
+            if (more)
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) load(next[u], at + (BATCH + u) * BLOCK);
+#pragma unroll
+            for (int u = 0; u < BATCH; u += PAIR)
+                if (first + u * BLOCK < sp.hi) take(b + u, at + u * BLOCK, first + (u + PAIR) * BLOCK <= sp.hi);
+            if (!more) break;
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) b[u] = next[u];
+            at += BATCH * BLOCK;
+            first += BATCH * BLOCK;
+        }
     }
     if (tid < sp.edges) {
         const float x[1] = {element(row + sp.edge(tid, n))};
-        absorb<SUMS>(a, x, c, c1);
+        absorb<ALSO>(a, x, c);
     }
     if (own != nullptr) *own = a.m;
-    join<SUMS, BLOCK>(a, c, c1, lds);
+    join<ALSO, BLOCK>(a, c, lds);
     return a;
 }
 
@@ -186,7 +269,7 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
             const int who = t.thread[a];
             for (int c = sp.lo + who + lane * BLOCK; c < sp.hi; c += 64 * BLOCK) {
                 float x[V];
-                aligned_chunk(row, sp.first(c), x);
+                unpack<T>(raw_chunk<T, false>(row, sp.first(c)), x);
 #pragma unroll
                 for (int j = 0; j < V; ++j) offer(x[j], sp.first(c) + j);
             }
@@ -231,7 +314,8 @@ __global__ __launch_bounds__(BLOCK) void logprob_forward_kernel(const T *__restr
     const T *row = logits + r * ld;
     const RowSplit<T> sp(row, n);
     float own;
-    const Sums a = row_sums<T, BLOCK, ENTROPY ? 2 : 1>(row, n, sp, c, 0.f, &own, lds);
+    uint4 none[1];
+    const Sums a = row_sums<T, BLOCK, ENTROPY ? Z_TIMES : NOTHING, true, 0>(row, n, sp, c, &own, lds, none);
     const float lns = logf(a.s);
     if (threadIdx.x == 0) {
         if (ENTROPY) entropy[r] = a.m == -INFINITY && a.s == 0.f ? 0.f : lns - LN2 * a.t / a.s;
@@ -286,6 +370,15 @@ template <typename T, int BLOCK, int MOST> struct ListedOut {
         for (int e = 0; e < EACH; ++e) {
             const int i = threadIdx.x + e * BLOCK;
             if (i < count && l.at[i] >= from && l.at[i] < to) x[e] = element(in + l.at[i]);
+        }
+    }
+    __device__ __forceinline__ void read(const T *in, int n, const ListLds<MOST> &l, int count)  // of the whole row
+    {
+        from = 0, to = n;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int i = threadIdx.x + e * BLOCK;
+            if (i < count && l.at[i] >= 0 && l.at[i] < n) x[e] = element(in + l.at[i]);
         }
     }
     template <typename F> __device__ __forceinline__ void write(T *out, const ListLds<MOST> &l, int count, F value)
@@ -365,9 +458,6 @@ int launch_logprob_backward(const LogitsArgs &a, const int64_t *targets, int giv
                                 : logprob_backward<float>(a, targets, given, dlogprob, dentropy, entropy, stats, (float *)out, ld_out, s);
 }
 
-size_t logprob_workspace(int, int64_t, int64_t, int) { return 0; }
-size_t distill_workspace(int, int64_t, int64_t) { return 0; }
-
 // Threads per row: one wavefront for short rows, so that many rows share a compute unit without barriers; 1024 where the
 // rows are too few to occupy the chip otherwise.
 static int row_block(const LogitsArgs &a)
@@ -392,7 +482,7 @@ static int row_block(const LogitsArgs &a)
     } while (0)
 
 int launch_logprob_forward(const LogitsArgs &a, const int64_t *targets, int given, float *logprob, float *entropy, int top, int64_t *top_index, float *top_logprob,
-                           float *stats, void *, hipStream_t s)
+                           float *stats, hipStream_t s)
 {
     ProfScope prof(KID_LOGPROB, s, 0.0, (double)a.rows * a.classes * elem_size(a.dtype));
     const float inv_t = 1.f / a.temperature, c = LOG2E / a.temperature;
@@ -502,10 +592,24 @@ template <int BLOCK, bool TWO> __device__ __forceinline__ Coefs row_coefs(const 
     return k;
 }
 
-// Whole rows: the loss, and with GRADIENT also the gradient, for which the row is read again while the caches hold it.
-template <typename T, int BLOCK, bool TWO, bool GRADIENT>
-__global__ __launch_bounds__(BLOCK) void distill_rows_kernel(const T *logits, int64_t ld, int64_t rows, int n, DistillArgs d, float *__restrict__ loss,
-                                                             float *__restrict__ stats, T *out, int64_t ld_out)
+// The gradient's value at x, ct 2^(zT) + c1 2^(z1).
+template <int ALSO> struct Gradient {
+    float m, c, ct, c1;
+    __device__ __forceinline__ Gradient(const Coefs &k, float max, float scale) : m(max == -INFINITY ? 0.f : max), c(scale), ct(ALSO == NOTHING ? k.ct + k.c1 : k.ct), c1(k.c1) {}
+    __device__ __forceinline__ float operator()(float x) const
+    {
+        const float d = x - m, e = exp2_fast(d * c);
+        if (ALSO == NOTHING) return e * ct;
+        if (ALSO == SQUARED) return e * fmaf(e, c1, ct);
+        if (ALSO == SQUARED2) return e * fmaf(e * e * e, c1, ct);
+        return e * ct + exp2_fast(d * LOG2E) * c1;
+    }
+};
+
+// Whole rows: the loss alone.
+template <typename T, int BLOCK, int ALSO>
+__global__ __launch_bounds__(BLOCK) void distill_loss_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int n, DistillArgs d, float c, float *__restrict__ loss,
+                                                             float *__restrict__ stats)
 {
     __shared__ float lds[2 * (BLOCK / 64)];
     __shared__ EntryLds l;
@@ -513,34 +617,64 @@ __global__ __launch_bounds__(BLOCK) void distill_rows_kernel(const T *logits, in
     if (r >= rows) return;
     const T *row = logits + r * ld;
     const RowSplit<T> sp(row, n);
-    const float t = d.alpha > 0.f && d.kept > 0 ? d.temperature : 1.f, c = LOG2E / t;
-    const Sums a = row_sums<T, BLOCK, TWO ? -1 : 1>(row, n, sp, c, LOG2E, nullptr, lds);
+    uint4 none[1];
+    const Sums a = row_sums<T, BLOCK, ALSO, true, 0>(row, n, sp, c, nullptr, lds, none);
     const Entries e = read_entries<BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
     __syncthreads();
-    const float v = row_loss<T, BLOCK, TWO>(d, row, r, n, a, e, l, lds);
+    const float v = row_loss<T, BLOCK, ALSO != NOTHING>(d, row, r, n, a, e, l, lds);
     if (threadIdx.x == 0) {
-        if (loss != nullptr) loss[r] = v;
-        if (stats != nullptr) stats[4 * r] = a.m, stats[4 * r + 1] = a.s, stats[4 * r + 2] = TWO ? a.t : a.s, stats[4 * r + 3] = 0.f;
+        loss[r] = v;
+        if (stats != nullptr) stats[4 * r] = a.m, stats[4 * r + 1] = a.s, stats[4 * r + 2] = ALSO != NOTHING ? a.t : a.s, stats[4 * r + 3] = 0.f;
     }
-    if (!GRADIENT) return;
+}
+
+// Loss and gradient of whole rows.  The row's first KEPT chunks a thread stay in registers from the sums to the gradient; what
+// a longer row has beyond them is read again.
+template <typename T, int BLOCK, int KEPT, int ALSO>
+__global__ __launch_bounds__(BLOCK) void distill_both_kernel(const T *logits, int64_t ld, int64_t rows, int n, DistillArgs d, float c, float *__restrict__ loss, T *out,
+                                                             int64_t ld_out)
+{
+    constexpr int V = CHUNK<T>;
+    __shared__ float lds[2 * (BLOCK / 64)];
+    __shared__ EntryLds l;
+    const int64_t r = grid_row();
+    if (r >= rows) return;
+    const T *row = logits + r * ld;
     T *to = out + r * ld_out;
-    const Coefs k = row_coefs<BLOCK, TWO>(d, r, n, a.m, a.s, a.t, e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
-    const float m0 = a.m == -INFINITY ? 0.f : a.m, ct = TWO ? k.ct : k.ct + k.c1;
-    auto value = [&](float x) {
-        const float z = x - m0;
-        return TWO ? exp2_fast(z * c) * ct + exp2_fast(z * LOG2E) * k.c1 : exp2_fast(z * c) * ct;
-    };
-    ListedOut<T, BLOCK, KEPT_MOST + 1> listed;
-    const int64_t chunks = (n + CHUNK<T> - 1) / CHUNK<T> + 1;
-    listed.read(row, to, n, 0, chunks, l, k.count);
+    const RowSplit<T> sp(row, n);
+    uint4 kept[KEPT];
+    const Sums a = row_sums<T, BLOCK, ALSO, false, KEPT>(row, n, sp, c, nullptr, lds, kept);
+    const Entries e = read_entries<BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
     __syncthreads();
-    write_row<T, BLOCK>(row, to, n, 0, chunks, value);
+    const float v = row_loss<T, BLOCK, ALSO != NOTHING>(d, row, r, n, a, e, l, lds);
+    if (threadIdx.x == 0) loss[r] = v;
+    const Coefs k = row_coefs<BLOCK, ALSO != NOTHING>(d, r, n, a.m, a.s, a.t, e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
+    const Gradient<ALSO> value(k, a.m, c);
+    ListedOut<T, BLOCK, KEPT_MOST + 1> listed;
+    listed.read(row, n, l, k.count);
+    const float edge = (int)threadIdx.x < sp.edges ? element(row + sp.edge(threadIdx.x, n)) : 0.f;
+    __syncthreads();
+    auto put = [&](const uint4 &b, int c) {
+        float x[V];
+        unpack<T>(b, x);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = value(x[j]);
+        ChunkBits<T> w;
+        pack(x, w.w);
+        *reinterpret_cast<ChunkBits<T> *>(to + sp.first(c)) = w;
+    };
+    int at = sp.lo + threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < KEPT; ++u)
+        if (at + u * BLOCK < sp.hi) put(kept[u], at + u * BLOCK);
+    for (at += KEPT * BLOCK; at < sp.hi; at += BLOCK) put(raw_chunk<T, false>(row, sp.first(at)), at);
+    if ((int)threadIdx.x < sp.edges) set_element(to + sp.edge(threadIdx.x, n), value(edge));
     __syncthreads();
     listed.write(to, l, k.count, value);
 }
 
-template <typename T, bool TWO>
-__global__ __launch_bounds__(GRAD_BLOCK) void distill_backward_kernel(const T *logits, int64_t ld, int64_t rows, int n, int pieces, DistillArgs d,
+template <typename T, int ALSO>
+__global__ __launch_bounds__(GRAD_BLOCK) void distill_backward_kernel(const T *logits, int64_t ld, int64_t rows, int n, int pieces, DistillArgs d, float c,
                                                                       const float *__restrict__ stats, T *out, int64_t ld_out)
 {
     __shared__ float lds[2 * (GRAD_BLOCK / 64)];
@@ -550,15 +684,11 @@ __global__ __launch_bounds__(GRAD_BLOCK) void distill_backward_kernel(const T *l
     const int64_t c0 = (id % pieces) * GRAD_CHUNKS, c1 = c0 + GRAD_CHUNKS;
     const T *in = logits + r * ld;
     T *to = out + r * ld_out;
-    const float t = d.alpha > 0.f && d.kept > 0 ? d.temperature : 1.f, c = LOG2E / t, m = stats[4 * r];
+    const float m = stats[4 * r];
     const Entries e = read_entries<GRAD_BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
     __syncthreads();
-    const Coefs k = row_coefs<GRAD_BLOCK, TWO>(d, r, n, m, stats[4 * r + 1], stats[4 * r + 2], e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
-    const float m0 = m == -INFINITY ? 0.f : m, ct = TWO ? k.ct : k.ct + k.c1;
-    auto value = [&](float x) {
-        const float z = x - m0;
-        return TWO ? exp2_fast(z * c) * ct + exp2_fast(z * LOG2E) * k.c1 : exp2_fast(z * c) * ct;
-    };
+    const Coefs k = row_coefs<GRAD_BLOCK, ALSO != NOTHING>(d, r, n, m, stats[4 * r + 1], stats[4 * r + 2], e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
+    const Gradient<ALSO> value(k, m, c);
     ListedOut<T, GRAD_BLOCK, KEPT_MOST + 1> listed;
     listed.read(in, to, n, c0, c1, l, k.count);
     __syncthreads();
@@ -567,38 +697,70 @@ __global__ __launch_bounds__(GRAD_BLOCK) void distill_backward_kernel(const T *l
     listed.write(to, l, k.count, value);
 }
 
-// two exponentials an element: both losses are there, at different temperatures
-static bool two_softmaxes(const DistillArgs &d) { return d.alpha > 0.f && d.alpha < 1.f && d.kept > 0 && d.labels != nullptr && d.temperature != 1.f; }
-
-int launch_distill_rows(const LogitsArgs &a, const DistillArgs &d, float *loss, float *stats, void *out, int64_t ld_out, void *, hipStream_t s)
+// What t holds: the second softmax is there only where both losses are, at different temperatures.  T = 2 and T = 4 take it as a
+// power of the first, in one or two products instead of an exponential, four issue slots.
+static Also second_softmax(const DistillArgs &d)
 {
-    ProfScope prof(KID_DISTILL, s, 0.0, (out != nullptr ? 2.0 : 1.0) * (double)a.rows * a.classes * elem_size(a.dtype));
-    const bool two = two_softmaxes(d);
-#define OMNI_DISTILL_ROWS(T, B, TWO, G) \
-    hipLaunchKernelGGL((distill_rows_kernel<T, B, TWO, G>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, d, loss, stats, (T *)out, ld_out)
-#define OMNI_DISTILL(T, B)                                                    \
-    do {                                                                      \
-        if (two && out != nullptr) OMNI_DISTILL_ROWS(T, B, true, true);       \
-        else if (two) OMNI_DISTILL_ROWS(T, B, true, false);                   \
-        else if (out != nullptr) OMNI_DISTILL_ROWS(T, B, false, true);        \
-        else OMNI_DISTILL_ROWS(T, B, false, false);                           \
+    if (!(d.alpha > 0.f && d.alpha < 1.f && d.kept > 0 && d.labels != nullptr && d.temperature != 1.f)) return NOTHING;
+    return d.temperature == 2.f ? SQUARED : d.temperature == 4.f ? SQUARED2 : AT_ONE;
+}
+
+#define OMNI_BY_SECOND(LAUNCH, ...)                           \
+    do {                                                      \
+        const Also also = second_softmax(d);                  \
+        if (also == NOTHING) LAUNCH(__VA_ARGS__, NOTHING);    \
+        else if (also == SQUARED) LAUNCH(__VA_ARGS__, SQUARED); \
+        else if (also == SQUARED2) LAUNCH(__VA_ARGS__, SQUARED2); \
+        else LAUNCH(__VA_ARGS__, AT_ONE);                     \
     } while (0)
-    OMNI_BY_TYPE_AND_BLOCK(OMNI_DISTILL);
-#undef OMNI_DISTILL
-#undef OMNI_DISTILL_ROWS
+
+static float distill_scale(const DistillArgs &d) { return LOG2E / (d.alpha > 0.f && d.kept > 0 ? d.temperature : 1.f); }
+
+int launch_distill_loss(const LogitsArgs &a, const DistillArgs &d, float *loss, float *stats, hipStream_t s)
+{
+    ProfScope prof(KID_DISTILL, s, 0.0, (double)a.rows * a.classes * elem_size(a.dtype));
+    const float c = distill_scale(d);
+#define OMNI_DISTILL_LOSS(T, B, ALSO) \
+    hipLaunchKernelGGL((distill_loss_kernel<T, B, ALSO>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, d, c, loss, stats)
+#define OMNI_DISTILL_LOSS2(T, B) OMNI_BY_SECOND(OMNI_DISTILL_LOSS, T, B)
+    OMNI_BY_TYPE_AND_BLOCK(OMNI_DISTILL_LOSS2);
+#undef OMNI_DISTILL_LOSS2
+#undef OMNI_DISTILL_LOSS
     OMNI_LAUNCH_CHECK();
     return OMNI_OK;
 }
 
+template <typename T> static int distill_both(const LogitsArgs &a, const DistillArgs &d, float *loss, T *out, int64_t ld_out, hipStream_t s)
+{
+    const float c = distill_scale(d);
+    const int64_t chunks = a.classes / CHUNK<T>;
+#define OMNI_DISTILL_BOTH(B, K, ALSO) \
+    hipLaunchKernelGGL((distill_both_kernel<T, B, K, ALSO>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, d, c, loss, out, ld_out)
+    if (chunks <= 256) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 64, 4);
+    else if (chunks <= 1024) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 256, 4);
+    else if (chunks <= 4096) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 256, 16);
+    else if (chunks <= 8192) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 512, 16);
+    else OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 1024, 16);
+#undef OMNI_DISTILL_BOTH
+    OMNI_LAUNCH_CHECK();
+    return OMNI_OK;
+}
+
+int launch_distill_both(const LogitsArgs &a, const DistillArgs &d, float *loss, void *out, int64_t ld_out, hipStream_t s)
+{
+    ProfScope prof(KID_DISTILL, s, 0.0, 2.0 * (double)a.rows * a.classes * elem_size(a.dtype));
+    return a.dtype == OMNI_BF16 ? distill_both<bf16_t>(a, d, loss, (bf16_t *)out, ld_out, s) : distill_both<float>(a, d, loss, (float *)out, ld_out, s);
+}
+
 template <typename T> static int distill_backward(const LogitsArgs &a, const DistillArgs &d, const float *stats, T *out, int64_t ld_out, hipStream_t s)
 {
+    const float c = distill_scale(d);
     const int pieces = (int)(((a.classes + CHUNK<T> - 1) / CHUNK<T> + 1 + GRAD_CHUNKS - 1) / GRAD_CHUNKS);
-    if (two_softmaxes(d))
-        hipLaunchKernelGGL((distill_backward_kernel<T, true>), row_grid(a.rows * pieces), dim3(GRAD_BLOCK), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, d, stats,
-                           out, ld_out);
-    else
-        hipLaunchKernelGGL((distill_backward_kernel<T, false>), row_grid(a.rows * pieces), dim3(GRAD_BLOCK), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, d, stats,
-                           out, ld_out);
+#define OMNI_DISTILL_BACKWARD(B, ALSO)                                                                                                                              \
+    hipLaunchKernelGGL((distill_backward_kernel<T, ALSO>), row_grid(a.rows * pieces), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, d, c, stats, \
+                       out, ld_out)
+    OMNI_BY_SECOND(OMNI_DISTILL_BACKWARD, GRAD_BLOCK);
+#undef OMNI_DISTILL_BACKWARD
     OMNI_LAUNCH_CHECK();
     return OMNI_OK;
 }

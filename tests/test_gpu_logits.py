@@ -372,12 +372,10 @@ def test_together_on_other_streams_and_in_a_replayed_graph(B):
     index, best = torch.empty((rows, k), dtype=torch.int64, device="cuda"), torch.empty((rows, k), device="cuda")
     loss, out = torch.empty(rows, device="cuda"), torch.empty_like(student)
     lp, h, st = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty((rows, 2), device="cuda")
-    ws = [torch.empty(max(16, b), dtype=torch.uint8, device="cuda") for b in
-          (B.logprob_workspace_bytes(rows, n, k, torch.bfloat16), B.distill_workspace_bytes(rows, n, torch.bfloat16))]
 
     def together():
-        B.logprob_forward(big, labels, k, logprob=lp, entropy=h, top_index=index, top_logprob=best, stats=st, workspace=ws[0])
-        B.distill_forward_backward(student, index, best, labels, 2.0, 0.5, dloss=w, loss=loss, dlogits=out, workspace=ws[1])
+        B.logprob_forward(big, labels, k, logprob=lp, entropy=h, top_index=index, top_logprob=best, stats=st)
+        B.distill_forward_backward(student, index, best, labels, 2.0, 0.5, dloss=w, loss=loss, dlogits=out)
         B.logprob_backward(student, st, labels, w, dlogits=big)          # (with the teacher's sums: only its repetition is looked at)
     outs = (index, best, loss, out, lp, h, st, big)
     side = torch.cuda.Stream()
