@@ -1,164 +1,368 @@
 // Layer norm over the rows of a matrix, forward and backward with the reduction of the weights' gradients (gfx950).
 //   mu = mean x, r = (mean (x - mu)^2 + eps)^-1/2, xh = (x - mu) r, y = xh gamma + beta
 //   g = dy gamma:  dx = r (g - mean g - xh mean(g xh)),  dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
-// A few operations an element: bound by HBM traffic.
+// A few operations an element: bound by memory.
 #include "row_ops.h"
 
 namespace omni {
 
-// One workgroup per row.  The row stays in registers between its three uses (mean, squares about the mean, output) where
-// BLOCK * CHUNKS chunks hold it; CHUNKS == 0: a longer row is read three times, the second and third time from the caches.
+// The sums of N values over the TEAM threads that share a row, to each of them.  lds [N][16] is this join's own: a later join
+// with another buffer lies between two uses of one, so one barrier is enough.
+template <int TEAM, int N> __device__ __forceinline__ void team_join(float (&v)[N], float (*lds)[16])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_join(v[i], Add());
+    if (TEAM == 64) return;
+    constexpr int WAVES = TEAM / 64;
+    const int wave = threadIdx.x / 64, first = wave / WAVES * WAVES;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) lds[i][wave] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float r = lds[i][first];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) r += lds[i][first + w];
+        v[i] = r;
+    }
+}
+
+// CHUNK floats of a vector over the columns, or `fill`
+template <int V> __device__ __forceinline__ void load_columns(const float *p, int at, int n, float fill, float (&v)[V])
+{
+    if (p != nullptr && at + V <= n) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+            const float4 f = *reinterpret_cast<const float4 *>(p + at + j);
+            v[j] = f.x, v[j + 1] = f.y, v[j + 2] = f.z, v[j + 3] = f.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = p != nullptr && at + j < n ? p[at + j] : fill;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ forward
+// BLOCK threads per row, CHUNKS chunks each, which stay in registers between the row's three uses (mean, squares about the mean,
+// output); a workgroup goes on to further rows with gamma and beta in registers too and the next row's loads in flight, since
+// from the caches the two of them are 8 bytes an element where a bf16 element itself is 4, read and written.
 // The squares are summed about the mean, not as mean x^2 - mu^2, which cancels where |mu| is large against the spread.
 template <typename T, int BLOCK, int CHUNKS>
 __global__ __launch_bounds__(BLOCK) void layer_norm_forward_kernel(const T *x, int64_t ldx, int64_t rows, int n, float eps, const float *__restrict__ gamma,
                                                                    const float *__restrict__ beta, T *y, int64_t ldy, float *__restrict__ mean, float *__restrict__ rstd)
 {
-    constexpr int V = CHUNK<T>, KEPT = CHUNKS > 0 ? CHUNKS : 1;
-    __shared__ float lds[BLOCK / 64];
+    constexpr int V = CHUNK<T>;
+    __shared__ float lds[2][1][16];
+    const int tid = threadIdx.x;
+    const float inv_n = 1.0f / (float)n;
+    float ga[CHUNKS][V], be[CHUNKS][V];
+    Raw<T> next[CHUNKS];
+    int64_t r = grid_row();
+    if (r >= rows) return;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        next[c] = load_raw(x + r * ldx, (c * BLOCK + tid) * V, n);
+        load_columns<V>(gamma, (c * BLOCK + tid) * V, n, 1.f, ga[c]);
+        load_columns<V>(beta, (c * BLOCK + tid) * V, n, 0.f, be[c]);
+    }
+    for (;;) {
+        float v[CHUNKS][V], sum[1] = {0.f}, sq[1] = {0.f};
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) unpack(next[c].w, v[c]);
+        const int64_t r2 = r + (int64_t)gridDim.x * gridDim.y;
+        if (r2 < rows)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) next[c] = load_raw(x + r2 * ldx, (c * BLOCK + tid) * V, n);
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum[0] += v[c][j];
+        team_join<BLOCK>(sum, lds[0]);
+        const float mu = sum[0] / (float)n;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                v[c][j] -= mu;
+                if ((c * BLOCK + tid) * V + j < n) sq[0] += v[c][j] * v[c][j];
+            }
+        team_join<BLOCK>(sq, lds[1]);
+        const float rs = 1.0f / sqrtf(sq[0] / (float)n + eps);
+        if (tid == 0) {
+            if (mean != nullptr) mean[r] = mu;
+            if (rstd != nullptr) rstd[r] = rs;
+        }
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[c][j] = v[c][j] * rs * ga[c][j] + be[c][j];
+            store_chunk(y + r * ldy, (c * BLOCK + tid) * V, n, v[c]);
+        }
+        if (r2 >= rows) return;
+        r = r2;
+    }
+}
+
+// Rows too long for that are read three times, the second and third time from the caches.
+template <typename T>
+__global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T *x, int64_t ldx, int64_t rows, int n, float eps, const float *__restrict__ gamma,
+                                                                       const float *__restrict__ beta, T *y, int64_t ldy, float *__restrict__ mean, float *__restrict__ rstd)
+{
+    constexpr int V = CHUNK<T>;
+    __shared__ float lds[2][1][16];
     const int64_t r = grid_row();
     if (r >= rows) return;
     const T *row = x + r * ldx;
-    T *out = y + r * ldy;
-    const int chunks = CHUNKS > 0 ? CHUNKS : (n + BLOCK * V - 1) / (BLOCK * V);
-    float v[KEPT][V], sum[1] = {0.f};
-    for (int c = 0; c < chunks; ++c) {
-        float(&w)[V] = v[CHUNKS > 0 ? c : 0];
-        load_chunk(row, (c * BLOCK + (int)threadIdx.x) * V, n, 0.f, w);
+    float v[V], w[V], sum[1] = {0.f}, sq[1] = {0.f};
+    for (int at = threadIdx.x * V; at < n; at += 1024 * V) {
+        load_chunk(row, at, n, 0.f, v);
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum[0] += w[j];
+        for (int j = 0; j < V; ++j) sum[0] += v[j];
     }
-    block_join<BLOCK>(sum, lds, Add());
+    team_join<1024>(sum, lds[0]);
     const float mu = sum[0] / (float)n;
-    sum[0] = 0.f;
-    for (int c = 0; c < chunks; ++c) {
-        const int at = (c * BLOCK + (int)threadIdx.x) * V;
-        float(&w)[V] = v[CHUNKS > 0 ? c : 0];
-        if (CHUNKS == 0) load_chunk(row, at, n, 0.f, w);
+    for (int at = threadIdx.x * V; at < n; at += 1024 * V) {
+        load_chunk(row, at, n, mu, v);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float d = at + j < n ? w[j] - mu : 0.f;
-            sum[0] += d * d;
-        }
+        for (int j = 0; j < V; ++j) sq[0] += (v[j] - mu) * (v[j] - mu);
     }
-    block_join<BLOCK>(sum, lds, Add());
-    const float rs = 1.0f / sqrtf(sum[0] / (float)n + eps);
+    team_join<1024>(sq, lds[1]);
+    const float rs = 1.0f / sqrtf(sq[0] / (float)n + eps);
     if (threadIdx.x == 0) {
         if (mean != nullptr) mean[r] = mu;
         if (rstd != nullptr) rstd[r] = rs;
     }
-    for (int c = 0; c < chunks; ++c) {
-        const int at = (c * BLOCK + (int)threadIdx.x) * V;
-        float(&w)[V] = v[CHUNKS > 0 ? c : 0], ga[V], be[V];
-        if (at >= n) break;
-        if (CHUNKS == 0) load_chunk(row, at, n, 0.f, w);
+    for (int at = threadIdx.x * V; at < n; at += 1024 * V) {
+        load_chunk(row, at, n, 0.f, v);
+        load_columns<V>(gamma, at, n, 1.f, w);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            ga[j] = gamma != nullptr && at + j < n ? gamma[at + j] : 1.f;
-            be[j] = beta != nullptr && at + j < n ? beta[at + j] : 0.f;
-        }
+        for (int j = 0; j < V; ++j) v[j] = (v[j] - mu) * rs * w[j];
+        load_columns<V>(beta, at, n, 0.f, w);
 #pragma unroll
-        for (int j = 0; j < V; ++j) w[j] = (w[j] - mu) * rs * ga[j] + be[j];
-        store_chunk(out, at, n, w);
+        for (int j = 0; j < V; ++j) v[j] += w[j];
+        store_chunk(y + r * ldy, at, n, v);
     }
 }
 
-// The data gradient, one workgroup per row, x and dy in registers between the sums and the output in the same way.
-template <typename T, int BLOCK, int CHUNKS>
-__global__ __launch_bounds__(BLOCK) void layer_norm_dx_kernel(const T *x, int64_t ldx, const T *dy, int64_t lddy, int64_t rows, int n, const float *__restrict__ gamma,
-                                                              const float *__restrict__ mean, const float *__restrict__ rstd, T *dx, int64_t lddx)
-{
-    constexpr int V = CHUNK<T>, KEPT = CHUNKS > 0 ? CHUNKS : 1;
-    __shared__ float lds[2 * (BLOCK / 64)];
-    const int64_t r = grid_row();
-    if (r >= rows) return;
-    const T *xr = x + r * ldx, *dr = dy + r * lddy;
-    T *out = dx + r * lddx;
-    const float mu = mean[r], rs = rstd[r];
-    const int chunks = CHUNKS > 0 ? CHUNKS : (n + BLOCK * V - 1) / (BLOCK * V);
-    float xh[KEPT][V], g[KEPT][V], sums[2] = {0.f, 0.f};
-    auto take = [&](int at, float(&a)[V], float(&b)[V]) {
-        load_chunk(xr, at, n, mu, a);
-        load_chunk(dr, at, n, 0.f, b);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            a[j] = (a[j] - mu) * rs;
-            if (gamma != nullptr && at + j < n) b[j] *= gamma[at + j];
-        }
-    };
-    for (int c = 0; c < chunks; ++c) {
-        float(&a)[V] = xh[CHUNKS > 0 ? c : 0], (&b)[V] = g[CHUNKS > 0 ? c : 0];
-        take((c * BLOCK + (int)threadIdx.x) * V, a, b);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            sums[0] += b[j];
-            sums[1] += b[j] * a[j];
-        }
-    }
-    block_join<BLOCK>(sums, lds, Add());
-    const float mg = sums[0] / (float)n, mgx = sums[1] / (float)n;
-    for (int c = 0; c < chunks; ++c) {
-        const int at = (c * BLOCK + (int)threadIdx.x) * V;
-        if (at >= n) break;
-        float(&a)[V] = xh[CHUNKS > 0 ? c : 0], (&b)[V] = g[CHUNKS > 0 ? c : 0], o[V];
-        if (CHUNKS == 0) take(at, a, b);
-#pragma unroll
-        for (int j = 0; j < V; ++j) o[j] = rs * (b[j] - mg - a[j] * mgx);
-        store_chunk(out, at, n, o);
-    }
-}
+// ------------------------------------------------------------------------------------------------ backward
+template <typename T> struct NormBackward {
+    const T *x, *dy;
+    int64_t ldx, lddy, rows;
+    int n;
+    const float *gamma, *mean, *rstd;
+    T *dx;
+    int64_t lddx;
+    float *dgamma, *dbeta, *part;  // part [ranges or workgroups][2][n], null: the sums go to dgamma and dbeta themselves
+    int tiles;                     // tiles of columns
+    int64_t range;                 // rows of a range
+};
 
-// dgamma and dbeta: a workgroup adds LN_COLS chunks of columns over one range of rows, 256 / LN_COLS rows at a time, and
-// joins them in LDS; `part` [ranges][2][n] receives the range's sums (one range: they go straight to dgamma and dbeta).
-constexpr int LN_COLS = 8;
+constexpr int LN_TILE = 8;  // chunks across a tile of columns: 128 bytes of a row, a cache line
 
-template <typename T>
-__global__ __launch_bounds__(256) void layer_norm_weights_kernel(const T *__restrict__ x, int64_t ldx, const T *__restrict__ dy, int64_t lddy, int64_t rows, int n,
-                                                                 const float *__restrict__ mean, const float *__restrict__ rstd, int64_t range, float *__restrict__ part,
-                                                                 float *__restrict__ dgamma, float *__restrict__ dbeta)
+// The weights' gradients of one tile of columns over one range of rows by a workgroup of 1024: 128 rows at a time.
+template <typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, int tile, int64_t which, float (*lds)[2 * CHUNK<T>][LN_TILE])
 {
-    constexpr int V = CHUNK<T>, LANES = 256 / LN_COLS;
-    __shared__ float lds[2][V][256 + 8];
-    const int col = threadIdx.x % LN_COLS, lane = threadIdx.x / LN_COLS, at = (blockIdx.x * LN_COLS + col) * V;
-    const int64_t r0 = blockIdx.y * range, r1 = r0 + range < rows ? r0 + range : rows;
-    float ga[V], be[V];
+    constexpr int V = CHUNK<T>, LANES = 1024 / LN_TILE;
+    const int col = threadIdx.x % LN_TILE, lane = threadIdx.x / LN_TILE, at = (tile * LN_TILE + col) * V;
+    const int64_t r1 = (which + 1) * a.range < a.rows ? (which + 1) * a.range : a.rows;
+    float s[2 * V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) ga[j] = be[j] = 0.f;
-    if (at < n)
-        for (int64_t r = r0 + lane; r < r1; r += LANES) {
-            const float mu = mean[r], rs = rstd[r];
-            float a[V], b[V];
-            load_chunk(x + r * ldx, at, n, mu, a);
-            load_chunk(dy + r * lddy, at, n, 0.f, b);
+    for (int j = 0; j < 2 * V; ++j) s[j] = 0.f;
+    if (at < a.n)
+#pragma unroll 4
+        for (int64_t r = which * a.range + lane; r < r1; r += LANES) {
+            const float mu = a.mean[r], rs = a.rstd[r];
+            float x[V], d[V];
+            load_chunk(a.x + r * a.ldx, at, a.n, mu, x);
+            load_chunk(a.dy + r * a.lddy, at, a.n, 0.f, d);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                ga[j] += b[j] * ((a[j] - mu) * rs);
-                be[j] += b[j];
+                s[j] += d[j] * ((x[j] - mu) * rs);
+                s[V + j] += d[j];
             }
         }
+    // the 8 rows of a wavefront, then the 16 wavefronts
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        lds[0][j][threadIdx.x] = ga[j];
-        lds[1][j][threadIdx.x] = be[j];
-    }
+    for (int j = 0; j < 2 * V; ++j)
+#pragma unroll
+        for (int off = LN_TILE; off < 64; off *= 2) s[j] += __shfl_xor(s[j], off, 64);
+    if ((threadIdx.x & 63) < LN_TILE)
+#pragma unroll
+        for (int j = 0; j < 2 * V; ++j) lds[threadIdx.x / 64][j][col] = s[j];
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * V * LN_COLS; i += 256) {
-        const int which = i / (V * LN_COLS), c = i / V % LN_COLS, j = i % V;
-        float s = 0.f;
-        for (int l = 0; l < LANES; ++l) s += lds[which][j][l * LN_COLS + c];
-        const int to = (blockIdx.x * LN_COLS + c) * V + j;
-        if (to >= n) continue;
-        if (part != nullptr) part[((int64_t)blockIdx.y * 2 + which) * n + to] = s;
-        else if (which == 0 && dgamma != nullptr) dgamma[to] = s;
-        else if (which == 1 && dbeta != nullptr) dbeta[to] = s;
+    if (threadIdx.x < 2 * V * LN_TILE) {
+        const int v = threadIdx.x / (V * LN_TILE), c = threadIdx.x / V % LN_TILE, j = threadIdx.x % V, to = (tile * LN_TILE + c) * V + j;
+        float r = 0.f;
+        for (int w = 0; w < 16; ++w) r += lds[w][v * V + j][c];
+        if (to < a.n) {
+            if (a.part != nullptr) a.part[(which * 2 + v) * a.n + to] = r;
+            else if (v == 0 && a.dgamma != nullptr) a.dgamma[to] = r;
+            else if (v == 1 && a.dbeta != nullptr) a.dbeta[to] = r;
+        }
     }
 }
 
-__global__ __launch_bounds__(256) void layer_norm_join_kernel(const float *__restrict__ part, int ranges, int n, float *__restrict__ dgamma, float *__restrict__ dbeta)
+// TEAM threads per row, 1024 / TEAM rows at a time, x and dy in registers between the sums and the output.  The first
+// tiles x ranges workgroups (`columns` of them) take the weights' gradients; the two kinds run beside each other, and what one
+// reads the other finds in the caches.  With WEIGHTS there are none of that kind: a workgroup goes on to further rows, the next
+// row's loads in flight, adds their part of the weights' gradients in registers and leaves its sums in `part`.
+template <typename T, int TEAM, int CHUNKS, bool WEIGHTS>
+__global__ __launch_bounds__(1024) void layer_norm_backward_kernel(NormBackward<T> a, int columns)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= 2 * (int64_t)n) return;
+    constexpr int V = CHUNK<T>, TEAMS = 1024 / TEAM;
+    __shared__ float lds[2][2][16];
+    __shared__ float sums[16][2 * V][LN_TILE];
+    if (!WEIGHTS && (int)blockIdx.x < columns) {
+        norm_columns(a, (int)blockIdx.x % a.tiles, blockIdx.x / a.tiles, sums);
+        return;
+    }
+    const int team = threadIdx.x / TEAM, lane = threadIdx.x % TEAM;
+    const int64_t step = (int64_t)(gridDim.x - columns) * TEAMS;
+    const float inv_n = 1.0f / (float)a.n;
+    float ga[CHUNKS][V], dg[CHUNKS][V], db[CHUNKS][V];
+    Raw<T> nx[CHUNKS], nd[CHUNKS];
+    float nmu = 0.f, nrs = 0.f;
+    auto fetch = [&](int64_t r) {  // (a row past the last one: zeros, which add nothing)
+        nmu = r < a.rows ? a.mean[r] : 0.f;
+        nrs = r < a.rows ? a.rstd[r] : 0.f;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int n = r < a.rows ? a.n : 0;
+            nx[c] = load_raw(a.x + r * a.ldx, (c * TEAM + lane) * V, n);
+            nd[c] = load_raw(a.dy + r * a.lddy, (c * TEAM + lane) * V, n);
+        }
+    };
+    int64_t r = (int64_t)(blockIdx.x - columns) * TEAMS + team;
+    fetch(r);
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        load_columns<V>(a.gamma, (c * TEAM + lane) * V, a.n, 1.f, ga[c]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) dg[c][j] = db[c][j] = 0.f;
+    }
+    for (int turn = 0;; turn ^= 1, r += step) {
+        float xh[CHUNKS][V], d[CHUNKS][V], s[2] = {0.f, 0.f};
+        const float mu = nmu, rs = nrs;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            unpack(nx[c].w, xh[c]);
+            unpack(nd[c].w, d[c]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) xh[c][j] = (c * TEAM + lane) * V + j < a.n ? (xh[c][j] - mu) * rs : 0.f;
+        }
+        const bool more = r - team + step < a.rows;  // (the same for the whole workgroup)
+        if (WEIGHTS && more) fetch(r + step);
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (WEIGHTS) {
+                    dg[c][j] += d[c][j] * xh[c][j];
+                    db[c][j] += d[c][j];
+                }
+                d[c][j] *= ga[c][j];
+                s[0] += d[c][j];
+                s[1] += d[c][j] * xh[c][j];
+            }
+        team_join<TEAM>(s, lds[turn]);
+        const float mg = s[0] * inv_n, mgx = s[1] * inv_n;
+        if (a.dx != nullptr && r < a.rows)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[c][j] = rs * (d[c][j] - mg - xh[c][j] * mgx);
+                store_chunk(a.dx + r * a.lddx, (c * TEAM + lane) * V, a.n, d[c]);
+            }
+        if (!more) break;
+    }
+    if (!WEIGHTS) return;
+    // the teams' sums, a team after the other
+    float *part = a.part + (int64_t)blockIdx.x * 2 * a.n;
+    extern __shared__ float rows_lds[];  // [2][CHUNKS][V][TEAM]
+    for (int t = TEAMS - 1; t > 0; --t) {
+        __syncthreads();
+        if (team == t)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    rows_lds[(c * V + j) * TEAM + lane] = dg[c][j];
+                    rows_lds[((CHUNKS + c) * V + j) * TEAM + lane] = db[c][j];
+                }
+        __syncthreads();
+        if (team == 0)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    dg[c][j] += rows_lds[(c * V + j) * TEAM + lane];
+                    db[c][j] += rows_lds[((CHUNKS + c) * V + j) * TEAM + lane];
+                }
+    }
+    if (team == 0)
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            store_floats<V>(part, (c * TEAM + lane) * V, a.n, dg[c]);
+            store_floats<V>(part + a.n, (c * TEAM + lane) * V, a.n, db[c]);
+        }
+}
+
+// Rows of more chunks than 1024 threads hold in registers: x and dy are read a second time from the caches.
+template <typename T> __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(NormBackward<T> a, int columns)
+{
+    constexpr int V = CHUNK<T>;
+    __shared__ float lds[2][16];
+    __shared__ float sums[16][2 * V][LN_TILE];
+    if ((int)blockIdx.x < columns) {
+        norm_columns(a, (int)blockIdx.x % a.tiles, blockIdx.x / a.tiles, sums);
+        return;
+    }
+    const int64_t r = blockIdx.x - columns;
+    const float mu = a.mean[r], rs = a.rstd[r];
+    float x[V], d[V], g[V], s[2] = {0.f, 0.f};
+    auto take = [&](int at) {
+        load_chunk(a.x + r * a.ldx, at, a.n, mu, x);
+        load_chunk(a.dy + r * a.lddy, at, a.n, 0.f, d);
+        load_columns<V>(a.gamma, at, a.n, 1.f, g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            x[j] = (x[j] - mu) * rs;
+            d[j] *= g[j];
+        }
+    };
+    for (int at = threadIdx.x * V; at < a.n; at += 1024 * V) {
+        take(at);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            s[0] += d[j];
+            s[1] += d[j] * x[j];
+        }
+    }
+    team_join<1024>(s, lds);
+    const float mg = s[0] / (float)a.n, mgx = s[1] / (float)a.n;
+    for (int at = threadIdx.x * V; at < a.n; at += 1024 * V) {
+        take(at);
+#pragma unroll
+        for (int j = 0; j < V; ++j) d[j] = rs * (d[j] - mg - x[j] * mgx);
+        store_chunk(a.dx + r * a.lddx, at, a.n, d);
+    }
+}
+
+// The sums of the parts, 64 columns by 16 parts at a time.
+__global__ __launch_bounds__(1024) void layer_norm_join_kernel(const float *__restrict__ part, int parts, int n, float *__restrict__ dgamma, float *__restrict__ dbeta)
+{
+    __shared__ float lds[16][64];
+    const int col = threadIdx.x % 64, lane = threadIdx.x / 64;
+    const int64_t i = (int64_t)blockIdx.x * 64 + col;
     float s = 0.f;
-    for (int k = 0; k < ranges; ++k) s += part[(int64_t)k * 2 * n + i];
+    if (i < 2 * (int64_t)n)
+#pragma unroll 8
+        for (int k = lane; k < parts; k += 16) s += part[(int64_t)k * 2 * n + i];
+    lds[lane][col] = s;
+    __syncthreads();
+    if (lane > 0 || i >= 2 * (int64_t)n) return;
+    for (int l = 1; l < 16; ++l) s += lds[l][col];
     if (i < n) {
         if (dgamma != nullptr) dgamma[i] = s;
     } else if (dbeta != nullptr) {
@@ -166,42 +370,54 @@ __global__ __launch_bounds__(256) void layer_norm_join_kernel(const float *__res
     }
 }
 
-// Ranges of rows of the weights' gradients: about four workgroups per compute unit, 64 rows each at least.  Never fewer for
-// more rows; no rows are one empty range, whose sums are zero.
-static int64_t weight_ranges(int dtype, int64_t rows, int64_t n)
+// ------------------------------------------------------------------------------------------------ host side
+// How the weights' gradients are added.  fused: by the workgroups that take the rows, whose sums (8 bytes a column and workgroup,
+// written and read once) are then less than x and dy read again; else beside them, by tiles of columns over ranges of rows.
+struct WeightsPlan { bool fused; int64_t parts, tiles; };
+
+static WeightsPlan weights_plan(int dtype, int64_t rows, int64_t n)
 {
-    const int64_t cols = LN_COLS * (16 / (int64_t)elem_size(dtype)), tiles = (n + cols - 1) / cols;
-    const int64_t most = (rows + 63) / 64, want = (1024 + tiles - 1) / tiles, ranges = want < most ? want : most;
-    return ranges > 1 ? ranges : 1;
+    const int64_t v = 16 / (int64_t)elem_size(dtype), chunks = (n + v - 1) / v;
+    WeightsPlan p = {false, 1, (chunks + LN_TILE - 1) / LN_TILE};
+    if (rows > 2048 && chunks <= 2048) {
+        p.fused = true;
+        p.parts = 256;  // one workgroup per compute unit
+        return p;
+    }
+    // about four workgroups per compute unit, 2048 rows each at least (16 turns)
+    const int64_t most = rows / 2048, want = (1024 + p.tiles - 1) / p.tiles;
+    p.parts = want < most ? want : most;
+    if (p.parts < 1) p.parts = 1;
+    return p;
 }
 
 size_t layer_norm_workspace(int dtype, int64_t rows, int64_t n)
 {
-    const int64_t ranges = weight_ranges(dtype, rows, n);
-    return ranges > 1 ? (size_t)ranges * 2 * n * sizeof(float) : 0;
+    // what fewer rows need is never more: 256 parts where rows > 2048, else at most rows / 2048
+    const WeightsPlan p = weights_plan(dtype, rows, n);
+    return p.fused || p.parts > 1 ? (size_t)p.parts * 2 * n * sizeof(float) : 0;
 }
 
-// BLOCK and CHUNKS by the row's length: the smallest workgroup that holds the row in at most four chunks a thread
-#define OMNI_LN_BY_LENGTH(LAUNCH)                          \
-    do {                                                   \
-        const int64_t chunks = (n + CHUNK<T> - 1) / CHUNK<T>; \
-        if (chunks <= 64) LAUNCH(64, 1);                   \
-        else if (chunks <= 256) LAUNCH(64, 4);             \
-        else if (chunks <= 512) LAUNCH(256, 2);            \
-        else if (chunks <= 1024) LAUNCH(256, 4);           \
-        else if (chunks <= 2048) LAUNCH(512, 4);           \
-        else if (chunks <= 4096) LAUNCH(1024, 4);          \
-        else LAUNCH(1024, 0);                              \
-    } while (0)
+template <typename T, int BLOCK, int CHUNKS>
+static void launch_forward(const LayerNormArgs &a, float eps, const float *beta, T *y, int64_t ldy, float *mean, float *rstd, hipStream_t s)
+{
+    // workgroups that are resident at once: 24 wavefronts per compute unit
+    const int64_t most = 256 * 24 / (BLOCK / 64);
+    hipLaunchKernelGGL((layer_norm_forward_kernel<T, BLOCK, CHUNKS>), row_grid(a.rows < most ? a.rows : most), dim3(BLOCK), 0, s, (const T *)a.x, a.ldx, a.rows, (int)a.width, eps,
+                       a.gamma, beta, y, ldy, mean, rstd);
+}
 
 template <typename T> static int forward(const LayerNormArgs &a, float eps, const float *beta, T *y, int64_t ldy, float *mean, float *rstd, hipStream_t s)
 {
-    const int64_t n = a.width;
-#define OMNI_LN_FORWARD(B, C)                                                                                                              \
-    hipLaunchKernelGGL((layer_norm_forward_kernel<T, B, C>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.x, a.ldx, a.rows, (int)n, eps, a.gamma, beta, \
-                       y, ldy, mean, rstd)
-    OMNI_LN_BY_LENGTH(OMNI_LN_FORWARD);
-#undef OMNI_LN_FORWARD
+    const int64_t chunks = (a.width + CHUNK<T> - 1) / CHUNK<T>;
+    if (chunks <= 64) launch_forward<T, 64, 1>(a, eps, beta, y, ldy, mean, rstd, s);
+    else if (chunks <= 128) launch_forward<T, 64, 2>(a, eps, beta, y, ldy, mean, rstd, s);
+    else if (chunks <= 256) launch_forward<T, 256, 1>(a, eps, beta, y, ldy, mean, rstd, s);
+    else if (chunks <= 512) launch_forward<T, 256, 2>(a, eps, beta, y, ldy, mean, rstd, s);
+    else if (chunks <= 1024) launch_forward<T, 512, 2>(a, eps, beta, y, ldy, mean, rstd, s);
+    else if (chunks <= 2048) launch_forward<T, 1024, 2>(a, eps, beta, y, ldy, mean, rstd, s);
+    else
+        hipLaunchKernelGGL(layer_norm_forward_long_kernel<T>, row_grid(a.rows), dim3(1024), 0, s, (const T *)a.x, a.ldx, a.rows, (int)a.width, eps, a.gamma, beta, y, ldy, mean, rstd);
     OMNI_LAUNCH_CHECK();
     return OMNI_OK;
 }
@@ -212,27 +428,50 @@ int launch_layer_norm_forward(const LayerNormArgs &a, float eps, const float *be
     return a.dtype == OMNI_BF16 ? forward<bf16_t>(a, eps, beta, (bf16_t *)y, ldy, mean, rstd, s) : forward<float>(a, eps, beta, (float *)y, ldy, mean, rstd, s);
 }
 
+template <typename T, int TEAM, int CHUNKS> static void launch_backward(const NormBackward<T> &b, bool fused, int64_t columns, int64_t parts, bool dx, hipStream_t s)
+{
+    constexpr int64_t TEAMS = 1024 / TEAM;
+    const int64_t groups = (b.rows + TEAMS - 1) / TEAMS;
+    if (fused)
+        hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, true>), dim3((unsigned)parts), dim3(1024), TEAMS > 1 ? 2 * CHUNKS * CHUNK<T> * TEAM * sizeof(float) : 0, s, b, 0);
+    else
+        hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, false>), dim3((unsigned)(columns + (dx ? groups : 0))), dim3(1024), 0, s, b, (int)columns);
+}
+
+template <typename T> static int backward_launch(const NormBackward<T> &b, bool fused, int64_t columns, int64_t parts, bool dx, hipStream_t s)
+{
+    const int64_t chunks = (b.n + CHUNK<T> - 1) / CHUNK<T>;
+    if (chunks <= 64) launch_backward<T, 64, 1>(b, fused, columns, parts, dx, s);
+    else if (chunks <= 128) launch_backward<T, 128, 1>(b, fused, columns, parts, dx, s);
+    else if (chunks <= 256) launch_backward<T, 256, 1>(b, fused, columns, parts, dx, s);
+    else if (chunks <= 512) launch_backward<T, 512, 1>(b, fused, columns, parts, dx, s);
+    else if (chunks <= 1024) launch_backward<T, 1024, 1>(b, fused, columns, parts, dx, s);
+    else if (chunks <= 2048) launch_backward<T, 1024, 2>(b, fused, columns, parts, dx, s);
+    else hipLaunchKernelGGL(layer_norm_backward_long_kernel<T>, dim3((unsigned)(columns + (dx ? b.rows : 0))), dim3(1024), 0, s, b, (int)columns);
+    OMNI_LAUNCH_CHECK();
+    return OMNI_OK;
+}
+
 template <typename T>
 static int backward(const LayerNormArgs &a, const T *dy, int64_t lddy, const float *mean, const float *rstd, T *dx, int64_t lddx, float *dgamma, float *dbeta, float *part,
                     hipStream_t s)
 {
-    const int64_t n = a.width;
-    const T *x = (const T *)a.x;
-    if (dgamma != nullptr || dbeta != nullptr) {  // first: dx may be written over x or dy
-        const int64_t ranges = weight_ranges(a.dtype, a.rows, n), range = (a.rows + ranges - 1) / ranges, cols = LN_COLS * CHUNK<T>;
-        hipLaunchKernelGGL(layer_norm_weights_kernel<T>, dim3((unsigned)((n + cols - 1) / cols), (unsigned)ranges), dim3(256), 0, s, x, a.ldx, dy, lddy, a.rows, (int)n,
-                           mean, rstd, range, ranges > 1 ? part : nullptr, dgamma, dbeta);
-        OMNI_LAUNCH_CHECK();
-        if (ranges > 1) {
-            hipLaunchKernelGGL(layer_norm_join_kernel, dim3((unsigned)((2 * n + 255) / 256)), dim3(256), 0, s, part, (int)ranges, (int)n, dgamma, dbeta);
-            OMNI_LAUNCH_CHECK();
-        }
+    const bool weights = dgamma != nullptr || dbeta != nullptr;
+    WeightsPlan p = weights_plan(a.dtype, a.rows, a.width);
+    const int64_t range = p.fused || p.parts == 0 ? a.rows : (a.rows + p.parts - 1) / p.parts, columns = p.tiles * p.parts;
+    NormBackward<T> b = {(const T *)a.x, dy, a.ldx, lddy, a.rows, (int)a.width, a.gamma, mean, rstd, dx, lddx, dgamma, dbeta, p.parts > 1 ? part : nullptr, (int)p.tiles, range};
+    int st;
+    if (!weights) return dx != nullptr ? backward_launch(b, false, 0, 0, true, s) : OMNI_OK;
+    if (p.fused) {
+        if ((st = backward_launch(b, true, 0, p.parts, true, s)) != OMNI_OK) return st;
+    } else if (dx != nullptr && ((const void *)dx == a.x || dx == dy)) {  // dx is written over what the sums are taken from: after them
+        if ((st = backward_launch(b, false, columns, 0, false, s)) != OMNI_OK) return st;
+        if ((st = backward_launch(b, false, 0, 0, true, s)) != OMNI_OK) return st;
+    } else if ((st = backward_launch(b, false, columns, 0, dx != nullptr, s)) != OMNI_OK) {
+        return st;
     }
-    if (dx != nullptr) {
-#define OMNI_LN_DX(B, C) \
-    hipLaunchKernelGGL((layer_norm_dx_kernel<T, B, C>), row_grid(a.rows), dim3(B), 0, s, x, a.ldx, dy, lddy, a.rows, (int)n, a.gamma, mean, rstd, dx, lddx)
-        OMNI_LN_BY_LENGTH(OMNI_LN_DX);
-#undef OMNI_LN_DX
+    if (p.parts > 1) {
+        hipLaunchKernelGGL(layer_norm_join_kernel, dim3((unsigned)((2 * a.width + 63) / 64)), dim3(1024), 0, s, part, (int)p.parts, (int)a.width, dgamma, dbeta);
         OMNI_LAUNCH_CHECK();
     }
     return OMNI_OK;

@@ -51,6 +51,27 @@ template <typename T> __device__ __forceinline__ void load_chunk(const T *row, i
         for (int j = 0; j < CHUNK<T>; ++j) v[j] = at + j >= 0 && at + j < n ? element(row + at + j) : fill;
     }
 }
+// The same, zero outside the row, as it lies in memory: for a chunk that is loaded long before it is used.
+template <typename T> using Raw = ChunkBits<T>;
+template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *row, int at, int n)
+{
+    Raw<T> b = {{0, 0, 0, 0}};
+    if (at + CHUNK<T> <= n) {
+        b = *reinterpret_cast<const ChunkBits<T> *>(row + at);
+    } else {
+        float v[CHUNK<T>];
+#pragma unroll
+        for (int j = 0; j < CHUNK<T>; ++j) v[j] = at + j < n ? element(row + at + j) : 0.f;
+        pack(v, b.w);
+    }
+    return b;
+}
+template <int V> __device__ __forceinline__ void store_floats(float *p, int at, int n, const float (&v)[V])
+{
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (at + j < n) p[at + j] = v[j];
+}
 template <typename T> __device__ __forceinline__ void store_chunk(T *row, int at, int n, const float (&v)[CHUNK<T>])
 {
     if (at >= 0 && at + CHUNK<T> <= n) {
