@@ -48,14 +48,13 @@ template <int V> __device__ __forceinline__ void load_columns(const float *p, in
 // output); a workgroup goes on to further rows with gamma and beta in registers too and the next row's loads in flight, since
 // from the caches the two of them are 8 bytes an element where a bf16 element itself is 4, read and written.
 // The squares are summed about the mean, not as mean x^2 - mu^2, which cancels where |mu| is large against the spread.
-template <typename T, int BLOCK, int CHUNKS>
-__global__ __launch_bounds__(BLOCK) void layer_norm_forward_kernel(const T *x, int64_t ldx, int64_t rows, int n, float eps, const float *__restrict__ gamma,
+template <typename T, int BLOCK, int CHUNKS, bool CUT>
+__global__ __launch_bounds__(BLOCK, BLOCK <= 512 ? 6 : 4) void layer_norm_forward_kernel(const T *x, int64_t ldx, int64_t rows, int n, float eps, const float *__restrict__ gamma,
                                                                    const float *__restrict__ beta, T *y, int64_t ldy, float *__restrict__ mean, float *__restrict__ rstd)
 {
     constexpr int V = CHUNK<T>;
     __shared__ float lds[2][1][16];
     const int tid = threadIdx.x;
-    const float inv_n = 1.0f / (float)n;
     float ga[CHUNKS][V], be[CHUNKS][V];
     Raw<T> next[CHUNKS];
     int64_t r = grid_row();
@@ -69,7 +68,10 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_forward_kernel(const T *x, i
     for (;;) {
         float v[CHUNKS][V], sum[1] = {0.f}, sq[1] = {0.f};
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) unpack(next[c].w, v[c]);
+        for (int c = 0; c < CHUNKS; ++c) {
+            settle<CUT>(next[c], (c * BLOCK + tid) * V, n);
+            unpack(next[c].w, v[c]);
+        }
         const int64_t r2 = r + (int64_t)gridDim.x * gridDim.y;
         if (r2 < rows)
 #pragma unroll
@@ -81,12 +83,16 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_forward_kernel(const T *x, i
         team_join<BLOCK>(sum, lds[0]);
         const float mu = sum[0] / (float)n;
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c)
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int at = (c * BLOCK + tid) * V;
+            float q = 0.f;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 v[c][j] -= mu;
-                if ((c * BLOCK + tid) * V + j < n) sq[0] += v[c][j] * v[c][j];
+                if (!CUT || at + j < n) q += v[c][j] * v[c][j];
             }
+            sq[0] += CUT || at < n ? q : 0.f;
+        }
         team_join<BLOCK>(sq, lds[1]);
         const float rs = 1.0f / sqrtf(sq[0] / (float)n + eps);
         if (tid == 0) {
@@ -104,37 +110,61 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_forward_kernel(const T *x, i
     }
 }
 
-// Rows too long for that are read three times, the second and third time from the caches.
+// Longer rows: a workgroup of 1024 per row, which keeps the first LONG_KEPT chunks a thread as they lie in memory; what a row has
+// beyond them is read three times, the second and third time from the caches.
+constexpr int LONG_KEPT = 8;
+
 template <typename T>
 __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T *x, int64_t ldx, int64_t rows, int n, float eps, const float *__restrict__ gamma,
                                                                        const float *__restrict__ beta, T *y, int64_t ldy, float *__restrict__ mean, float *__restrict__ rstd)
 {
-    constexpr int V = CHUNK<T>;
+    constexpr int V = CHUNK<T>, STEP = 1024 * V;
     __shared__ float lds[2][1][16];
     const int64_t r = grid_row();
     if (r >= rows) return;
     const T *row = x + r * ldx;
-    float v[V], w[V], sum[1] = {0.f}, sq[1] = {0.f};
-    for (int at = threadIdx.x * V; at < n; at += 1024 * V) {
-        load_chunk(row, at, n, 0.f, v);
+    const int first = threadIdx.x * V;
+    Raw<T> kept[LONG_KEPT];
+    float sum[1] = {0.f}, sq[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < LONG_KEPT; ++c) kept[c] = load_raw(row, first + c * STEP, n);
+    // f(v, at) for every chunk of the thread that begins inside the row, zero outside it
+    auto each = [&](auto f) {
+        float v[V];
+#pragma unroll
+        for (int c = 0; c < LONG_KEPT; ++c)
+            if (first + c * STEP < n) {
+                unpack(kept[c].w, v);
+                f(v, first + c * STEP);
+            }
+        for (int at = first + LONG_KEPT * STEP; at < n; at += STEP) {
+            load_chunk(row, at, n, 0.f, v);
+            f(v, at);
+        }
+    };
+#pragma unroll
+    for (int c = 0; c < LONG_KEPT; ++c) settle<true>(kept[c], first + c * STEP, n);
+    each([&](float(&v)[V], int) {
 #pragma unroll
         for (int j = 0; j < V; ++j) sum[0] += v[j];
-    }
+    });
     team_join<1024>(sum, lds[0]);
     const float mu = sum[0] / (float)n;
-    for (int at = threadIdx.x * V; at < n; at += 1024 * V) {
-        load_chunk(row, at, n, mu, v);
+    each([&](float(&v)[V], int at) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) sq[0] += (v[j] - mu) * (v[j] - mu);
-    }
+        for (int j = 0; j < V; ++j) {
+            const float d = at + j < n ? v[j] - mu : 0.f;
+            sq[0] += d * d;
+        }
+    });
     team_join<1024>(sq, lds[1]);
     const float rs = 1.0f / sqrtf(sq[0] / (float)n + eps);
     if (threadIdx.x == 0) {
         if (mean != nullptr) mean[r] = mu;
         if (rstd != nullptr) rstd[r] = rs;
     }
-    for (int at = threadIdx.x * V; at < n; at += 1024 * V) {
-        load_chunk(row, at, n, 0.f, v);
+    each([&](float(&v)[V], int at) {
+        float w[V];
         load_columns<V>(gamma, at, n, 1.f, w);
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = (v[j] - mu) * rs * w[j];
@@ -142,7 +172,7 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T *
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] += w[j];
         store_chunk(y + r * ldy, at, n, v);
-    }
+    });
 }
 
 // ------------------------------------------------------------------------------------------------ backward
@@ -154,47 +184,59 @@ template <typename T> struct NormBackward {
     T *dx;
     int64_t lddx;
     float *dgamma, *dbeta, *part;  // part [ranges or workgroups][2][n], null: the sums go to dgamma and dbeta themselves
-    int tiles;                     // tiles of columns
+    int tiles, narrow;             // tiles of columns, and whether they are of 2 chunks
     int64_t range;                 // rows of a range
 };
 
-constexpr int LN_TILE = 8;  // chunks across a tile of columns: 128 bytes of a row, a cache line
-
-// The weights' gradients of one tile of columns over one range of rows by a workgroup of 1024: 128 rows at a time.
-template <typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, int tile, int64_t which, float (*lds)[2 * CHUNK<T>][LN_TILE])
+// The weights' gradients of one tile of columns, TILE chunks across, over one range of rows by a workgroup of 1024: 1024 / TILE
+// rows at a time, four of them a thread in flight.
+template <int TILE, typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, int tile, int64_t which, float *lds)
 {
-    constexpr int V = CHUNK<T>, LANES = 1024 / LN_TILE;
-    const int col = threadIdx.x % LN_TILE, lane = threadIdx.x / LN_TILE, at = (tile * LN_TILE + col) * V;
+    constexpr int V = CHUNK<T>, LANES = 1024 / TILE, ROWS = 4;
+    const int col = threadIdx.x % TILE, lane = threadIdx.x / TILE, at = (tile * TILE + col) * V;
     const int64_t r1 = (which + 1) * a.range < a.rows ? (which + 1) * a.range : a.rows;
     float s[2 * V];
 #pragma unroll
     for (int j = 0; j < 2 * V; ++j) s[j] = 0.f;
-    if (at < a.n)
-#pragma unroll 4
-        for (int64_t r = which * a.range + lane; r < r1; r += LANES) {
-            const float mu = a.mean[r], rs = a.rstd[r];
-            float x[V], d[V];
-            load_chunk(a.x + r * a.ldx, at, a.n, mu, x);
-            load_chunk(a.dy + r * a.lddy, at, a.n, 0.f, d);
+    for (int64_t r = which * a.range + lane; r < r1; r += ROWS * LANES) {
+        Raw<T> x[ROWS], d[ROWS];
+        float mu[ROWS], rs[ROWS];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int64_t k = r + i * LANES < r1 ? r + i * LANES : r;
+            x[i] = load_raw(a.x + k * a.ldx, at, a.n);
+            d[i] = load_raw(a.dy + k * a.lddy, at, a.n);
+            mu[i] = a.mean[k];
+            rs[i] = a.rstd[k];
+        }
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            if (r + i * LANES >= r1) break;
+            float xv[V], dv[V];
+            settle<true>(x[i], at, a.n);
+            settle<true>(d[i], at, a.n);
+            unpack(x[i].w, xv);
+            unpack(d[i].w, dv);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                s[j] += d[j] * ((x[j] - mu) * rs);
-                s[V + j] += d[j];
+                s[j] += dv[j] * ((xv[j] - mu[i]) * rs[i]);
+                s[V + j] += dv[j];
             }
         }
-    // the 8 rows of a wavefront, then the 16 wavefronts
+    }
+    // the rows of a wavefront, then the 16 wavefronts: lds [16][2 V][TILE]
 #pragma unroll
     for (int j = 0; j < 2 * V; ++j)
 #pragma unroll
-        for (int off = LN_TILE; off < 64; off *= 2) s[j] += __shfl_xor(s[j], off, 64);
-    if ((threadIdx.x & 63) < LN_TILE)
+        for (int off = TILE; off < 64; off *= 2) s[j] += __shfl_xor(s[j], off, 64);
+    if ((threadIdx.x & 63) < TILE)
 #pragma unroll
-        for (int j = 0; j < 2 * V; ++j) lds[threadIdx.x / 64][j][col] = s[j];
+        for (int j = 0; j < 2 * V; ++j) lds[((threadIdx.x / 64) * 2 * V + j) * TILE + col] = s[j];
     __syncthreads();
-    if (threadIdx.x < 2 * V * LN_TILE) {
-        const int v = threadIdx.x / (V * LN_TILE), c = threadIdx.x / V % LN_TILE, j = threadIdx.x % V, to = (tile * LN_TILE + c) * V + j;
+    if (threadIdx.x < 2 * V * TILE) {
+        const int v = threadIdx.x / (V * TILE), c = threadIdx.x / V % TILE, j = threadIdx.x % V, to = (tile * TILE + c) * V + j;
         float r = 0.f;
-        for (int w = 0; w < 16; ++w) r += lds[w][v * V + j][c];
+        for (int w = 0; w < 16; ++w) r += lds[(w * 2 * V + v * V + j) * TILE + c];
         if (to < a.n) {
             if (a.part != nullptr) a.part[(which * 2 + v) * a.n + to] = r;
             else if (v == 0 && a.dgamma != nullptr) a.dgamma[to] = r;
@@ -203,38 +245,51 @@ template <typename T> __device__ __forceinline__ void norm_columns(const NormBac
     }
 }
 
+// Tiles of 8 chunks, 128 bytes of a row and so a cache line, where there are enough of them to occupy the chip, else of 2.
+constexpr int LN_TILE = 8, LN_NARROW = 2, LN_LDS = 16 * 2 * 8 * LN_TILE;
+template <typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, float *lds)
+{
+    const int tile = (int)blockIdx.x % a.tiles, which = (int)blockIdx.x / a.tiles;
+    if (a.narrow) norm_columns<LN_NARROW>(a, tile, which, lds);
+    else norm_columns<LN_TILE>(a, tile, which, lds);
+}
+
 // TEAM threads per row, 1024 / TEAM rows at a time, x and dy in registers between the sums and the output.  The first
 // tiles x ranges workgroups (`columns` of them) take the weights' gradients; the two kinds run beside each other, and what one
 // reads the other finds in the caches.  With WEIGHTS there are none of that kind: a workgroup goes on to further rows, the next
 // row's loads in flight, adds their part of the weights' gradients in registers and leaves its sums in `part`.
-template <typename T, int TEAM, int CHUNKS, bool WEIGHTS>
-__global__ __launch_bounds__(1024) void layer_norm_backward_kernel(NormBackward<T> a, int columns)
+template <typename T, int TEAM, int CHUNKS, bool WEIGHTS, bool CUT>
+__global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(4, 4))) void layer_norm_backward_kernel(NormBackward<T> a, int columns)
 {
     constexpr int V = CHUNK<T>, TEAMS = 1024 / TEAM;
     __shared__ float lds[2][2][16];
-    __shared__ float sums[16][2 * V][LN_TILE];
+    __shared__ float sums[WEIGHTS ? 1 : LN_LDS];
     if (!WEIGHTS && (int)blockIdx.x < columns) {
-        norm_columns(a, (int)blockIdx.x % a.tiles, blockIdx.x / a.tiles, sums);
+        norm_columns(a, sums);
         return;
     }
     const int team = threadIdx.x / TEAM, lane = threadIdx.x % TEAM;
     const int64_t step = (int64_t)(gridDim.x - columns) * TEAMS;
     const float inv_n = 1.0f / (float)a.n;
     float ga[CHUNKS][V], dg[CHUNKS][V], db[CHUNKS][V];
-    Raw<T> nx[CHUNKS], nd[CHUNKS];
-    float nmu = 0.f, nrs = 0.f;
-    auto fetch = [&](int64_t r) {  // (a row past the last one: zeros, which add nothing)
-        nmu = r < a.rows ? a.mean[r] : 0.f;
-        nrs = r < a.rows ? a.rstd[r] : 0.f;
+    // rows in flight: two in fp32 (8192 x 4096: 95 us with one, 80 with two), whose chunks are half as many values (16384 x 4096 bf16:
+    // 82 us with one, 95 with two)
+    constexpr int AHEAD = WEIGHTS && V == 4 && CHUNKS == 1 ? 2 : 1;
+    Raw<T> nx[AHEAD][CHUNKS], nd[AHEAD][CHUNKS];
+    float nmu[AHEAD], nrs[AHEAD];
+    auto fetch = [&](int i, int64_t r) {  // (a row past the last one: zeros, which add nothing)
+        nmu[i] = r < a.rows ? a.mean[r] : 0.f;
+        nrs[i] = r < a.rows ? a.rstd[r] : 0.f;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             const int n = r < a.rows ? a.n : 0;
-            nx[c] = load_raw(a.x + r * a.ldx, (c * TEAM + lane) * V, n);
-            nd[c] = load_raw(a.dy + r * a.lddy, (c * TEAM + lane) * V, n);
+            nx[i][c] = load_raw(a.x + r * a.ldx, (c * TEAM + lane) * V, n);
+            nd[i][c] = load_raw(a.dy + r * a.lddy, (c * TEAM + lane) * V, n);
         }
     };
     int64_t r = (int64_t)(blockIdx.x - columns) * TEAMS + team;
-    fetch(r);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) fetch(i, r + i * step);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         load_columns<V>(a.gamma, (c * TEAM + lane) * V, a.n, 1.f, ga[c]);
@@ -243,16 +298,26 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_kernel(NormBackward<
     }
     for (int turn = 0;; turn ^= 1, r += step) {
         float xh[CHUNKS][V], d[CHUNKS][V], s[2] = {0.f, 0.f};
-        const float mu = nmu, rs = nrs;
+        const float mu = nmu[0], rs = nrs[0];
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            unpack(nx[c].w, xh[c]);
-            unpack(nd[c].w, d[c]);
+            settle<CUT>(nx[0][c], (c * TEAM + lane) * V, a.n);
+            settle<CUT>(nd[0][c], (c * TEAM + lane) * V, a.n);
+            unpack(nx[0][c].w, xh[c]);
+            unpack(nd[0][c].w, d[c]);
 #pragma unroll
             for (int j = 0; j < V; ++j) xh[c][j] = (c * TEAM + lane) * V + j < a.n ? (xh[c][j] - mu) * rs : 0.f;
         }
         const bool more = r - team + step < a.rows;  // (the same for the whole workgroup)
-        if (WEIGHTS && more) fetch(r + step);
+        if (WEIGHTS && more) {
+#pragma unroll
+            for (int i = 0; i + 1 < AHEAD; ++i) {
+                nmu[i] = nmu[i + 1], nrs[i] = nrs[i + 1];
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) nx[i][c] = nx[i + 1][c], nd[i][c] = nd[i + 1][c];
+            }
+            fetch(AHEAD - 1, r + AHEAD * step);
+        }
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
@@ -276,7 +341,7 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_kernel(NormBackward<
             }
         if (!more) break;
     }
-    if (!WEIGHTS) return;
+    if (!WEIGHTS || a.part == nullptr) return;
     // the teams' sums, a team after the other
     float *part = a.part + (int64_t)blockIdx.x * 2 * a.n;
     extern __shared__ float rows_lds[];  // [2][CHUNKS][V][TEAM]
@@ -308,45 +373,72 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_kernel(NormBackward<
         }
 }
 
-// Rows of more chunks than 1024 threads hold in registers: x and dy are read a second time from the caches.
+// Rows of more chunks than that: the first LONG_KEPT chunks a thread of x and dy are kept as they lie in memory, what is beyond
+// them is read a second time from the caches.
 template <typename T> __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(NormBackward<T> a, int columns)
 {
-    constexpr int V = CHUNK<T>;
+    constexpr int V = CHUNK<T>, STEP = 1024 * V, KEPT = LONG_KEPT / 2;
     __shared__ float lds[2][16];
-    __shared__ float sums[16][2 * V][LN_TILE];
+    __shared__ float sums[LN_LDS];
     if ((int)blockIdx.x < columns) {
-        norm_columns(a, (int)blockIdx.x % a.tiles, blockIdx.x / a.tiles, sums);
+        norm_columns(a, sums);
         return;
     }
     const int64_t r = blockIdx.x - columns;
+    const T *xr = a.x + r * a.ldx, *dr = a.dy + r * a.lddy;
     const float mu = a.mean[r], rs = a.rstd[r];
-    float x[V], d[V], g[V], s[2] = {0.f, 0.f};
-    auto take = [&](int at) {
-        load_chunk(a.x + r * a.ldx, at, a.n, mu, x);
-        load_chunk(a.dy + r * a.lddy, at, a.n, 0.f, d);
-        load_columns<V>(a.gamma, at, a.n, 1.f, g);
+    const int first = threadIdx.x * V;
+    Raw<T> kx[KEPT], kd[KEPT];
+    float s[2] = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            x[j] = (x[j] - mu) * rs;
-            d[j] *= g[j];
+    for (int c = 0; c < KEPT; ++c) {
+        kx[c] = load_raw(xr, first + c * STEP, a.n);
+        kd[c] = load_raw(dr, first + c * STEP, a.n);
+    }
+    // f(xh, g, at) for every chunk of the thread; g is zero outside the row
+    auto each = [&](auto f) {
+        float x[V], d[V], g[V];
+        auto give = [&](int at) {
+            load_columns<V>(a.gamma, at, a.n, 1.f, g);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                x[j] = at + j < a.n ? (x[j] - mu) * rs : 0.f;
+                d[j] *= g[j];
+            }
+            f(x, d, at);
+        };
+#pragma unroll
+        for (int c = 0; c < KEPT; ++c)
+            if (first + c * STEP < a.n) {
+                unpack(kx[c].w, x);
+                unpack(kd[c].w, d);
+                give(first + c * STEP);
+            }
+        for (int at = first + KEPT * STEP; at < a.n; at += STEP) {
+            load_chunk(xr, at, a.n, 0.f, x);
+            load_chunk(dr, at, a.n, 0.f, d);
+            give(at);
         }
     };
-    for (int at = threadIdx.x * V; at < a.n; at += 1024 * V) {
-        take(at);
+#pragma unroll
+    for (int c = 0; c < KEPT; ++c) {
+        settle<true>(kx[c], first + c * STEP, a.n);
+        settle<true>(kd[c], first + c * STEP, a.n);
+    }
+    each([&](float(&x)[V], float(&d)[V], int) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             s[0] += d[j];
             s[1] += d[j] * x[j];
         }
-    }
+    });
     team_join<1024>(s, lds);
     const float mg = s[0] / (float)a.n, mgx = s[1] / (float)a.n;
-    for (int at = threadIdx.x * V; at < a.n; at += 1024 * V) {
-        take(at);
+    each([&](float(&x)[V], float(&d)[V], int at) {
 #pragma unroll
         for (int j = 0; j < V; ++j) d[j] = rs * (d[j] - mg - x[j] * mgx);
         store_chunk(a.dx + r * a.lddx, at, a.n, d);
-    }
+    });
 }
 
 // The sums of the parts, 64 columns by 16 parts at a time.
@@ -373,18 +465,19 @@ __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const float *__re
 // ------------------------------------------------------------------------------------------------ host side
 // How the weights' gradients are added.  fused: by the workgroups that take the rows, whose sums (8 bytes a column and workgroup,
 // written and read once) are then less than x and dy read again; else beside them, by tiles of columns over ranges of rows.
-struct WeightsPlan { bool fused; int64_t parts, tiles; };
+struct WeightsPlan { bool fused, narrow; int64_t parts, tiles; };
 
 static WeightsPlan weights_plan(int dtype, int64_t rows, int64_t n)
 {
     const int64_t v = 16 / (int64_t)elem_size(dtype), chunks = (n + v - 1) / v;
-    WeightsPlan p = {false, 1, (chunks + LN_TILE - 1) / LN_TILE};
+    WeightsPlan p = {false, chunks < 128 * LN_TILE, 1, 0};
+    p.tiles = p.narrow ? (chunks + LN_NARROW - 1) / LN_NARROW : (chunks + LN_TILE - 1) / LN_TILE;
     if (rows > 2048 && chunks <= 2048) {
         p.fused = true;
         p.parts = 256;  // one workgroup per compute unit
         return p;
     }
-    // about four workgroups per compute unit, 2048 rows each at least (16 turns)
+    // about four workgroups per compute unit, 2048 rows each at least
     const int64_t most = rows / 2048, want = (1024 + p.tiles - 1) / p.tiles;
     p.parts = want < most ? want : most;
     if (p.parts < 1) p.parts = 1;
@@ -402,9 +495,13 @@ template <typename T, int BLOCK, int CHUNKS>
 static void launch_forward(const LayerNormArgs &a, float eps, const float *beta, T *y, int64_t ldy, float *mean, float *rstd, hipStream_t s)
 {
     // workgroups that are resident at once: 24 wavefronts per compute unit
-    const int64_t most = 256 * 24 / (BLOCK / 64);
-    hipLaunchKernelGGL((layer_norm_forward_kernel<T, BLOCK, CHUNKS>), row_grid(a.rows < most ? a.rows : most), dim3(BLOCK), 0, s, (const T *)a.x, a.ldx, a.rows, (int)a.width, eps,
-                       a.gamma, beta, y, ldy, mean, rstd);
+    const int64_t most = 256 * (24 / (BLOCK / 64)), groups = a.rows < most ? a.rows : most;
+#define OMNI_LN_FORWARD(CUT)                                                                                                                                              \
+    hipLaunchKernelGGL((layer_norm_forward_kernel<T, BLOCK, CHUNKS, CUT>), row_grid(groups), dim3(BLOCK), 0, s, (const T *)a.x, a.ldx, a.rows, (int)a.width, eps, a.gamma, beta, y, \
+                       ldy, mean, rstd)
+    if (a.width % CHUNK<T> == 0) OMNI_LN_FORWARD(false);
+    else OMNI_LN_FORWARD(true);
+#undef OMNI_LN_FORWARD
 }
 
 template <typename T> static int forward(const LayerNormArgs &a, float eps, const float *beta, T *y, int64_t ldy, float *mean, float *rstd, hipStream_t s)
@@ -432,10 +529,10 @@ template <typename T, int TEAM, int CHUNKS> static void launch_backward(const No
 {
     constexpr int64_t TEAMS = 1024 / TEAM;
     const int64_t groups = (b.rows + TEAMS - 1) / TEAMS;
-    if (fused)
-        hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, true>), dim3((unsigned)parts), dim3(1024), TEAMS > 1 ? 2 * CHUNKS * CHUNK<T> * TEAM * sizeof(float) : 0, s, b, 0);
-    else
-        hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, false>), dim3((unsigned)(columns + (dx ? groups : 0))), dim3(1024), 0, s, b, (int)columns);
+    const size_t lds = TEAMS > 1 ? 2 * CHUNKS * CHUNK<T> * TEAM * sizeof(float) : 0;
+    if (!fused) hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, false, true>), dim3((unsigned)(columns + (dx ? groups : 0))), dim3(1024), 0, s, b, (int)columns);
+    else if (b.n % CHUNK<T> == 0) hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, true, false>), dim3((unsigned)parts), dim3(1024), lds, s, b, 0);
+    else hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, true, true>), dim3((unsigned)parts), dim3(1024), lds, s, b, 0);
 }
 
 template <typename T> static int backward_launch(const NormBackward<T> &b, bool fused, int64_t columns, int64_t parts, bool dx, hipStream_t s)
@@ -459,9 +556,12 @@ static int backward(const LayerNormArgs &a, const T *dy, int64_t lddy, const flo
     const bool weights = dgamma != nullptr || dbeta != nullptr;
     WeightsPlan p = weights_plan(a.dtype, a.rows, a.width);
     const int64_t range = p.fused || p.parts == 0 ? a.rows : (a.rows + p.parts - 1) / p.parts, columns = p.tiles * p.parts;
-    NormBackward<T> b = {(const T *)a.x, dy, a.ldx, lddy, a.rows, (int)a.width, a.gamma, mean, rstd, dx, lddx, dgamma, dbeta, p.parts > 1 ? part : nullptr, (int)p.tiles, range};
+    NormBackward<T> b = {(const T *)a.x, dy, a.ldx, lddy, a.rows, (int)a.width, a.gamma, mean, rstd, dx, lddx, dgamma, dbeta, p.parts > 1 ? part : nullptr, (int)p.tiles, p.narrow ? 1 : 0, range};
     int st;
-    if (!weights) return dx != nullptr ? backward_launch(b, false, 0, 0, true, s) : OMNI_OK;
+    if (!weights) {  // (the resident workgroups are the faster ones for many rows, also without sums to leave)
+        b.part = nullptr;
+        return backward_launch(b, p.fused, 0, p.parts, true, s);
+    }
     if (p.fused) {
         if ((st = backward_launch(b, true, 0, p.parts, true, s)) != OMNI_OK) return st;
     } else if (dx != nullptr && ((const void *)dx == a.x || dx == dy)) {  // dx is written over what the sums are taken from: after them

@@ -40,31 +40,61 @@ __device__ __forceinline__ float element(const bf16_t *p) { return bf16_to_f32(*
 __device__ __forceinline__ void set_element(float *p, float v) { *p = v; }
 __device__ __forceinline__ void set_element(bf16_t *p, float v) { *p = f32_to_bf16(v); }
 
-// Elements [at, at + CHUNK) of a row of n; those outside it are `fill`.
-template <typename T> __device__ __forceinline__ void load_chunk(const T *row, int at, int n, float fill, float (&v)[CHUNK<T>])
+// 16 bytes moved down by `bytes` (up, if negative), zero behind them
+__device__ __forceinline__ void shift_bytes(uint32_t (&w)[4], int bytes)
 {
-    if (at >= 0 && at + CHUNK<T> <= n) {
-        const ChunkBits<T> b = *reinterpret_cast<const ChunkBits<T> *>(row + at);
-        unpack(b.w, v);
-    } else {
-#pragma unroll
-        for (int j = 0; j < CHUNK<T>; ++j) v[j] = at + j >= 0 && at + j < n ? element(row + at + j) : fill;
+    uint64_t lo = w[0] | (uint64_t)w[1] << 32, hi = w[2] | (uint64_t)w[3] << 32;
+    if (bytes > 0) {
+        if (bytes >= 8) lo = hi, hi = 0;
+        const int k = bytes % 8 * 8;
+        if (k > 0) lo = lo >> k | hi << (64 - k), hi >>= k;
+    } else if (bytes < 0) {
+        if (bytes <= -8) hi = lo, lo = 0;
+        const int k = -bytes % 8 * 8;
+        if (k > 0) hi = hi << k | lo >> (64 - k), lo <<= k;
     }
+    w[0] = (uint32_t)lo, w[1] = (uint32_t)(lo >> 32), w[2] = (uint32_t)hi, w[3] = (uint32_t)(hi >> 32);
 }
-// The same, zero outside the row, as it lies in memory: for a chunk that is loaded long before it is used.
+
+// Elements [at, at + CHUNK) of a row of n as they lie in memory, zero outside the row, in two steps: load_raw starts the load,
+// settle is called where the chunk is used.  A chunk that is partly outside is cut from the row's first or last 16 bytes, which
+// are loaded whole: a load that needs a branch or its data at once keeps the loads around it from staying in flight (layer norm
+// of 8192 x 5001 bf16, whose rows end inside a chunk, with the cut at the load: forward 57 us, backward 95).
 template <typename T> using Raw = ChunkBits<T>;
 template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *row, int at, int n)
 {
+    constexpr int V = CHUNK<T>;
+    if (n >= V) return *reinterpret_cast<const ChunkBits<T> *>(row + (at < 0 ? 0 : at < n - V ? at : n - V));
     Raw<T> b = {{0, 0, 0, 0}};
-    if (at + CHUNK<T> <= n) {
-        b = *reinterpret_cast<const ChunkBits<T> *>(row + at);
-    } else {
-        float v[CHUNK<T>];
+    float v[V];
 #pragma unroll
-        for (int j = 0; j < CHUNK<T>; ++j) v[j] = at + j < n ? element(row + at + j) : 0.f;
-        pack(v, b.w);
-    }
+    for (int j = 0; j < V; ++j) v[j] = at + j >= 0 && at + j < n ? element(row + at + j) : 0.f;
+    pack(v, b.w);
     return b;
+}
+// CUT = false: n is a multiple of the chunk, so a chunk is inside or outside.
+template <bool CUT, typename T> __device__ __forceinline__ void settle(Raw<T> &b, int at, int n)
+{
+    constexpr int V = CHUNK<T>;
+    if (!CUT) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b.w[j] = at < n ? b.w[j] : 0;
+        return;
+    }
+    if ((at >= 0 && at + V <= n) || n < V) return;
+    if (at >= n || at + V <= 0) b = {{0, 0, 0, 0}};
+    else shift_bytes(b.w, (at < 0 ? at : at + V - n) * (int)sizeof(T));
+}
+// ... as floats; those outside the row are `fill`
+template <typename T> __device__ __forceinline__ void load_chunk(const T *row, int at, int n, float fill, float (&v)[CHUNK<T>])
+{
+    Raw<T> b = load_raw(row, at, n);
+    settle<true>(b, at, n);
+    unpack(b.w, v);
+    if (fill != 0.f && (at < 0 || at + CHUNK<T> > n))
+#pragma unroll
+        for (int j = 0; j < CHUNK<T>; ++j)
+            if (at + j < 0 || at + j >= n) v[j] = fill;
 }
 template <int V> __device__ __forceinline__ void store_floats(float *p, int at, int n, const float (&v)[V])
 {
@@ -98,12 +128,16 @@ template <int CTRL> __device__ __forceinline__ float dpp(float v)
 {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
 }
-template <typename OP> __device__ __forceinline__ float wave_join(float v, OP op)
+template <typename OP> __device__ __forceinline__ float join16(float v, OP op)  // over 16 lanes
 {
     v = op(v, dpp<0xb1>(v));   // quad_perm 1 0 3 2
     v = op(v, dpp<0x4e>(v));   // quad_perm 2 3 0 1
     v = op(v, dpp<0x141>(v));  // row_half_mirror
-    v = op(v, dpp<0x140>(v));  // row_mirror
+    return op(v, dpp<0x140>(v));  // row_mirror
+}
+template <typename OP> __device__ __forceinline__ float wave_join(float v, OP op)
+{
+    v = join16(v, op);
     auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
     auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
