@@ -12,6 +12,7 @@ fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 from pathlib import Path
 from typing import Optional, Sequence
 
@@ -553,10 +554,28 @@ def dropout_backward(dy, p: float, seed: int, stream_id: int = 0, dx=None):
 
 # ---------------------------------------------------------------- the end of a network
 # Matrices here are tensors [..., width] whose rows lie evenly spaced, each contiguous: a slice of a wider matrix is one.
-def _matrix(t: torch.Tensor, what: str):
+# A call on small matrices is as long as its host side (10 us of it, 3 the launch, when every tensor asked for the current device
+# and its shape several times), so each tensor is looked at once.
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_f32, _int64 = torch.float32, torch.int64
+
+
+def _device(t: torch.Tensor, what: str) -> int:
+    """The current GPU's number, where `t` has to live."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must live on the GPU")
+    return _current_device()
+
+
+def _matrix(t: torch.Tensor, dev: int, what: str):
     """(data_ptr, rows, width, ld) of a tensor on the current GPU."""
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    if t.get_device() != dev:
         raise ValueError(f"{what} must live on the current GPU")
+    if t.dim() == 2:
+        rows, width = t.shape
+        ld, step = t.stride()
+        if step == 1 and (ld >= width or rows < 2) and width > 0:
+            return t.data_ptr(), rows, width, ld if ld >= width else width
     if t.dim() == 0 or t.shape[-1] == 0:
         raise ValueError(f"{what} must have rows of at least one element")
     width = t.shape[-1]
@@ -578,36 +597,29 @@ def _matrix(t: torch.Tensor, what: str):
     return t.data_ptr(), rows, width, width if ld is None else max(ld, width)
 
 
-def _vector(t: Optional[torch.Tensor], count: int, dtype: torch.dtype, what: str) -> Optional[int]:
+def _vector(t: Optional[torch.Tensor], count: int, dtype: torch.dtype, dev: int, what: str) -> Optional[int]:
     """data_ptr of a dense tensor of `count` elements on the current GPU (None stays None)."""
     if t is None:
         return None
     if t.dtype is not dtype or t.numel() != count:
         raise ValueError(f"{what} must be {dtype} and hold {count} elements")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device() or not t.is_contiguous():
+    if t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous and live on the current GPU")
     return t.data_ptr()
 
 
-def _like(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, what: str):
-    p, r, w, ld = _matrix(t, what)
-    if (r, w) != (rows, width) or t.dtype is not dtype:
+def _like(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, dev: int, what: str):
+    p, r, w, ld = _matrix(t, dev, what)
+    if r != rows or w != width or t.dtype is not dtype:
         raise ValueError(f"{what} must be {dtype} with {rows} rows of {width}")
     return p, ld
 
 
-def _scratch(need: int, workspace: Optional[torch.Tensor], device):
-    """(pointer, bytes) of the caller's workspace, or of one that lives until the call returns (the allocator keeps its memory
-    for work queued behind it on the same stream)."""
-    if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    if workspace is None:
-        return None, 0, None
-    if not workspace.is_cuda or workspace.get_device() != torch.cuda.current_device() or not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous and live on the current GPU")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+def _stream_of(dev: int) -> int:
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
 
 
+@functools.lru_cache(maxsize=1024)
 def layer_norm_workspace_bytes(rows: int, width: int, dtype: torch.dtype = torch.float32) -> int:
     """omni_layer_norm_workspace_bytes: scratch of layer_norm_backward's weight gradients (0: none)."""
     b = _sz()
@@ -617,144 +629,161 @@ def layer_norm_workspace_bytes(rows: int, width: int, dtype: torch.dtype = torch
 
 def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, y=None, mean=None, rstd=None, want_stats: bool = True):
     """omni_layer_norm_forward over x's last axis; returns (y, mean, rstd) -- mean and rstd (fp32, one a row) are what
-    layer_norm_backward needs (None without want_stats)."""
-    px, rows, width, ldx = _matrix(x, "x")
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
-    py, ldy = _like(y, rows, width, x.dtype, "y")
+    layer_norm_backward needs (None without want_stats, unless they are given)."""
+    dev, dtype = _device(x, "x"), x.dtype
+    px, rows, width, ldx = _matrix(x, dev, "x")
+    if y is None:
+        y = torch.empty(x.shape, dtype=dtype, device=x.device)
+    py, ldy = _like(y, rows, width, dtype, dev, "y")
     if want_stats:
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
-    f32 = torch.float32
-    _check(_lib.omni_layer_norm_forward(dtype_code(x.dtype), rows, width, px, ldx, _vector(gamma, width, f32, "gamma"),
-                                        _vector(beta, width, f32, "beta"), eps, py, ldy, _vector(mean, rows, f32, "mean"),
-                                        _vector(rstd, rows, f32, "rstd"), _stream()))
+        if mean is None:
+            mean = torch.empty(x.shape[:-1], dtype=_f32, device=x.device)
+        if rstd is None:
+            rstd = torch.empty(x.shape[:-1], dtype=_f32, device=x.device)
+    _check(_lib.omni_layer_norm_forward(dtype_code(dtype), rows, width, px, ldx, _vector(gamma, width, _f32, dev, "gamma"),
+                                        _vector(beta, width, _f32, dev, "beta"), eps, py, ldy, _vector(mean, rows, _f32, dev, "mean"),
+                                        _vector(rstd, rows, _f32, dev, "rstd"), _stream_of(dev)))
     return y, mean, rstd
 
 
 def layer_norm_backward(x, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, want_dx: bool = True,
                         want_dweights: bool = True, workspace=None):
-    """omni_layer_norm_backward; returns (dx, dgamma, dbeta), dgamma and dbeta fp32 [width]."""
-    px, rows, width, ldx = _matrix(x, "x")
-    f32, code = torch.float32, dtype_code(x.dtype)
-    pdy, lddy = _like(dy, rows, width, x.dtype, "dy")
+    """omni_layer_norm_backward; returns (dx, dgamma, dbeta), dgamma and dbeta fp32 [width].  Without a workspace one is taken
+    from torch's allocator, which keeps its memory for the work queued on this stream."""
+    dev, dtype = _device(x, "x"), x.dtype
+    px, rows, width, ldx = _matrix(x, dev, "x")
+    pdy, lddy = _like(dy, rows, width, dtype, dev, "dy")
     if dx is None and want_dx:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    pdx, lddx = (None, 0) if dx is None else _like(dx, rows, width, x.dtype, "dx")
+        dx = torch.empty(x.shape, dtype=dtype, device=x.device)
+    pdx, lddx = (None, 0) if dx is None else _like(dx, rows, width, dtype, dev, "dx")
     if want_dweights:
-        dgamma = torch.empty((width,), dtype=f32, device=x.device) if dgamma is None else dgamma
-        dbeta = torch.empty((width,), dtype=f32, device=x.device) if dbeta is None else dbeta
-    need = 0
+        if dgamma is None:
+            dgamma = torch.empty((width,), dtype=_f32, device=x.device)
+        if dbeta is None:
+            dbeta = torch.empty((width,), dtype=_f32, device=x.device)
     if workspace is None and (dgamma is not None or dbeta is not None):
-        need = layer_norm_workspace_bytes(rows, width, x.dtype)
-    pw, nw, keep = _scratch(need, workspace, x.device)
-    _check(_lib.omni_layer_norm_backward(code, rows, width, px, ldx, pdy, lddy, _vector(gamma, width, f32, "gamma"),
-                                         _vector(mean, rows, f32, "mean"), _vector(rstd, rows, f32, "rstd"), pdx, lddx,
-                                         _vector(dgamma, width, f32, "dgamma"), _vector(dbeta, width, f32, "dbeta"), pw, nw, _stream()))
+        need = layer_norm_workspace_bytes(rows, width, dtype)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    pw, nw = None, 0
+    if workspace is not None:
+        nw = workspace.numel() * workspace.element_size()
+        pw = _vector(workspace, workspace.numel(), workspace.dtype, dev, "workspace")
+    _check(_lib.omni_layer_norm_backward(dtype_code(dtype), rows, width, px, ldx, pdy, lddy, _vector(gamma, width, _f32, dev, "gamma"),
+                                         _vector(mean, rows, _f32, dev, "mean"), _vector(rstd, rows, _f32, dev, "rstd"), pdx, lddx,
+                                         _vector(dgamma, width, _f32, dev, "dgamma"), _vector(dbeta, width, _f32, dev, "dbeta"), pw, nw,
+                                         _stream_of(dev)))
     return dx, dgamma, dbeta
 
 
-def _given(targets, rows: int) -> int:
-    if targets is None:
+def _per_row(t: Optional[torch.Tensor], rows: int, what: str) -> int:
+    """How many elements a row a tensor holds."""
+    if t is None or rows == 0:
         return 0
-    if rows and targets.numel() % rows:
-        raise ValueError("targets must hold the same number of classes for every row")
-    return targets.numel() // rows if rows else 0
+    n = t.numel()
+    if n % rows:
+        raise ValueError(f"{what} must hold the same number of elements for every row")
+    return n // rows
 
 
 def logprob_forward(logits, targets=None, top: int = 0, temperature: float = 1.0, logprob=None, entropy=None, top_index=None,
                     top_logprob=None, stats=None, want_entropy: bool = True, want_stats: bool = True):
     """omni_logprob_forward over logits [..., classes]; returns (logprob, entropy, top_index, top_logprob, stats).  targets:
     int64, any number of classes a row; logprob has targets' shape, entropy one value a row, top_index (int64) and top_logprob
-    `top` a row; stats is what logprob_backward needs."""
-    p, rows, classes, ld = _matrix(logits, "logits")
-    f32, i64, dev, lead, code = torch.float32, torch.int64, logits.device, tuple(logits.shape[:-1]), dtype_code(logits.dtype)
-    given = _given(targets, rows)
+    `top` a row; stats is what logprob_backward needs.  What is not asked for is None."""
+    dev = _device(logits, "logits")
+    p, rows, classes, ld = _matrix(logits, dev, "logits")
+    given = _per_row(targets, rows, "targets")
     if logprob is None and targets is not None:
-        logprob = torch.empty(targets.shape, dtype=f32, device=dev)
+        logprob = torch.empty(targets.shape, dtype=_f32, device=logits.device)
     if entropy is None and want_entropy:
-        entropy = torch.empty(lead, dtype=f32, device=dev)
+        entropy = torch.empty(logits.shape[:-1], dtype=_f32, device=logits.device)
     if top:
-        top_index = torch.empty(lead + (top,), dtype=i64, device=dev) if top_index is None else top_index
-        top_logprob = torch.empty(lead + (top,), dtype=f32, device=dev) if top_logprob is None else top_logprob
+        if top_index is None:
+            top_index = torch.empty(logits.shape[:-1] + (top,), dtype=_int64, device=logits.device)
+        if top_logprob is None:
+            top_logprob = torch.empty(logits.shape[:-1] + (top,), dtype=_f32, device=logits.device)
     if stats is None and want_stats:
-        stats = torch.empty(lead + (2,), dtype=f32, device=dev)
-    _check(_lib.omni_logprob_forward(code, rows, classes, p, ld, temperature, _vector(targets, rows * given, i64, "targets"), given,
-                                     _vector(logprob, rows * given, f32, "logprob"), _vector(entropy, rows, f32, "entropy"), top,
-                                     _vector(top_index, rows * top, i64, "top_index"), _vector(top_logprob, rows * top, f32, "top_logprob"),
-                                     _vector(stats, 2 * rows, f32, "stats"), _stream()))
+        stats = torch.empty(logits.shape[:-1] + (2,), dtype=_f32, device=logits.device)
+    _check(_lib.omni_logprob_forward(dtype_code(logits.dtype), rows, classes, p, ld, temperature,
+                                     _vector(targets, rows * given, _int64, dev, "targets"), given,
+                                     _vector(logprob, rows * given, _f32, dev, "logprob"), _vector(entropy, rows, _f32, dev, "entropy"), top,
+                                     _vector(top_index, rows * top, _int64, dev, "top_index"),
+                                     _vector(top_logprob, rows * top, _f32, dev, "top_logprob"),
+                                     _vector(stats, 2 * rows, _f32, dev, "stats"), _stream_of(dev)))
     return logprob, entropy, top_index, top_logprob, stats
 
 
 def logprob_backward(logits, stats, targets=None, dlogprob=None, dentropy=None, entropy=None, temperature: float = 1.0, dlogits=None):
     """omni_logprob_backward: gradient w.r.t. the logits, from dlogprob (targets' shape) and dentropy (one a row, with the
     entropy that logprob_forward gave)."""
-    p, rows, classes, ld = _matrix(logits, "logits")
-    f32, given = torch.float32, _given(targets, rows)
+    dev, dtype = _device(logits, "logits"), logits.dtype
+    p, rows, classes, ld = _matrix(logits, dev, "logits")
+    given = _per_row(targets, rows, "targets")
     if dlogits is None:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    po, ldo = _like(dlogits, rows, classes, logits.dtype, "dlogits")
-    _check(_lib.omni_logprob_backward(dtype_code(logits.dtype), rows, classes, p, ld, temperature, _vector(stats, 2 * rows, f32, "stats"),
-                                      _vector(targets, rows * given, torch.int64, "targets"), given,
-                                      _vector(dlogprob, rows * given, f32, "dlogprob"), _vector(dentropy, rows, f32, "dentropy"),
-                                      _vector(entropy, rows, f32, "entropy"), po, ldo, _stream()))
+        dlogits = torch.empty(logits.shape, dtype=dtype, device=logits.device)
+    po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits")
+    _check(_lib.omni_logprob_backward(dtype_code(dtype), rows, classes, p, ld, temperature, _vector(stats, 2 * rows, _f32, dev, "stats"),
+                                      _vector(targets, rows * given, _int64, dev, "targets"), given,
+                                      _vector(dlogprob, rows * given, _f32, dev, "dlogprob"), _vector(dentropy, rows, _f32, dev, "dentropy"),
+                                      _vector(entropy, rows, _f32, dev, "entropy"), po, ldo, _stream_of(dev)))
     return dlogits
 
 
-def _teacher(index, values, labels, rows: int):
+def _teacher(index, values, labels, rows: int, dev: int):
     """(index pointer, logits pointer, entries a row, labels pointer)"""
-    if (index is None) != (values is None):
-        raise ValueError("teacher_index and teacher_logits belong together")
-    kept = 0
-    if index is not None:
-        if index.shape != values.shape or (rows and index.numel() % rows):
-            raise ValueError("teacher_index and teacher_logits must hold the same number of entries for every row")
-        kept = index.numel() // rows if rows else 0
-    return (_vector(index, rows * kept, torch.int64, "teacher_index"), _vector(values, rows * kept, torch.float32, "teacher_logits"), kept,
-            _vector(labels, rows, torch.int64, "labels"))
+    kept = _per_row(index, rows, "teacher_index")
+    if (index is None) != (values is None) or (index is not None and index.shape != values.shape):
+        raise ValueError("teacher_index and teacher_logits must have the same shape")
+    return (_vector(index, rows * kept, _int64, dev, "teacher_index"), _vector(values, rows * kept, _f32, dev, "teacher_logits"), kept,
+            _vector(labels, rows, _int64, dev, "labels"))
 
 
 def distill_forward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0, loss=None,
                     stats=None, want_stats: bool = True):
     """omni_distill_forward over logits [..., classes]; returns (loss, stats): the loss of every row, and what distill_backward
     needs.  Without teacher entries (and alpha = 0) it is the labels' cross entropy."""
-    p, rows, classes, ld = _matrix(logits, "logits")
-    f32, dev = torch.float32, logits.device
-    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows)
-    loss = torch.empty(logits.shape[:-1], dtype=f32, device=dev) if loss is None else loss
+    dev = _device(logits, "logits")
+    p, rows, classes, ld = _matrix(logits, dev, "logits")
+    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows, dev)
+    if loss is None:
+        loss = torch.empty(logits.shape[:-1], dtype=_f32, device=logits.device)
     if stats is None and want_stats:
-        stats = torch.empty(tuple(logits.shape[:-1]) + (4,), dtype=f32, device=dev)
+        stats = torch.empty(logits.shape[:-1] + (4,), dtype=_f32, device=logits.device)
     _check(_lib.omni_distill_forward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                     _vector(loss, rows, f32, "loss"), _vector(stats, 4 * rows, f32, "stats"), _stream()))
+                                     _vector(loss, rows, _f32, dev, "loss"), _vector(stats, 4 * rows, _f32, dev, "stats"), _stream_of(dev)))
     return loss, stats
 
 
 def distill_backward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0, stats=None,
                      dloss=None, scale: float = 1.0, dlogits=None):
     """omni_distill_backward: gradient w.r.t. the logits of sum(scale * dloss * loss) (dloss: one a row; None: ones)."""
-    p, rows, classes, ld = _matrix(logits, "logits")
-    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows)
+    dev, dtype = _device(logits, "logits"), logits.dtype
+    p, rows, classes, ld = _matrix(logits, dev, "logits")
+    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows, dev)
     if dlogits is None:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    po, ldo = _like(dlogits, rows, classes, logits.dtype, "dlogits")
-    _check(_lib.omni_distill_backward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                      _vector(stats, 4 * rows, torch.float32, "stats"), _vector(dloss, rows, torch.float32, "dloss"), scale,
-                                      po, ldo, _stream()))
+        dlogits = torch.empty(logits.shape, dtype=dtype, device=logits.device)
+    po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits")
+    _check(_lib.omni_distill_backward(dtype_code(dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
+                                      _vector(stats, 4 * rows, _f32, dev, "stats"), _vector(dloss, rows, _f32, dev, "dloss"), scale,
+                                      po, ldo, _stream_of(dev)))
     return dlogits
 
 
 def distill_forward_backward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0,
                              dloss=None, scale: float = 1.0, loss=None, dlogits=None):
     """omni_distill_forward_backward: distill_forward and distill_backward in one call; returns (loss, dlogits)."""
-    p, rows, classes, ld = _matrix(logits, "logits")
-    f32, dev = torch.float32, logits.device
-    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows)
-    loss = torch.empty(logits.shape[:-1], dtype=f32, device=dev) if loss is None else loss
+    dev, dtype = _device(logits, "logits"), logits.dtype
+    p, rows, classes, ld = _matrix(logits, dev, "logits")
+    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows, dev)
+    if loss is None:
+        loss = torch.empty(logits.shape[:-1], dtype=_f32, device=logits.device)
     if dlogits is None:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-    po, ldo = _like(dlogits, rows, classes, logits.dtype, "dlogits")
-    _check(_lib.omni_distill_forward_backward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                              _vector(dloss, rows, f32, "dloss"), scale, _vector(loss, rows, f32, "loss"), po, ldo,
-                                              _stream()))
+        dlogits = torch.empty(logits.shape, dtype=dtype, device=logits.device)
+    po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits")
+    _check(_lib.omni_distill_forward_backward(dtype_code(dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
+                                              _vector(dloss, rows, _f32, dev, "dloss"), scale, _vector(loss, rows, _f32, dev, "loss"), po, ldo,
+                                              _stream_of(dev)))
     return loss, dlogits
 
 

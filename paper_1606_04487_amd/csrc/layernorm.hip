@@ -184,7 +184,7 @@ template <typename T> struct NormBackward {
     T *dx;
     int64_t lddx;
     float *dgamma, *dbeta, *part;  // part [ranges or workgroups][2][n], null: the sums go to dgamma and dbeta themselves
-    int tiles, narrow;             // tiles of columns, and whether they are of 2 chunks
+    int tiles, narrow;             // tiles of columns, and whether they are of 4 chunks
     int64_t range;                 // rows of a range
 };
 
@@ -226,9 +226,7 @@ template <int TILE, typename T> __device__ __forceinline__ void norm_columns(con
     }
     // the rows of a wavefront, then the 16 wavefronts: lds [16][2 V][TILE]
 #pragma unroll
-    for (int j = 0; j < 2 * V; ++j)
-#pragma unroll
-        for (int off = TILE; off < 64; off *= 2) s[j] += __shfl_xor(s[j], off, 64);
+    for (int j = 0; j < 2 * V; ++j) s[j] = join_strided<TILE>(s[j], Add());
     if ((threadIdx.x & 63) < TILE)
 #pragma unroll
         for (int j = 0; j < 2 * V; ++j) lds[((threadIdx.x / 64) * 2 * V + j) * TILE + col] = s[j];
@@ -245,8 +243,8 @@ template <int TILE, typename T> __device__ __forceinline__ void norm_columns(con
     }
 }
 
-// Tiles of 8 chunks, 128 bytes of a row and so a cache line, where there are enough of them to occupy the chip, else of 2.
-constexpr int LN_TILE = 8, LN_NARROW = 2, LN_LDS = 16 * 2 * 8 * LN_TILE;
+// Tiles of 8 chunks, 128 bytes of a row and so a cache line, where there are enough of them to occupy the chip, else of 4.
+constexpr int LN_TILE = 8, LN_NARROW = 4, LN_LDS = 16 * 2 * 8 * LN_TILE;
 template <typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, float *lds)
 {
     const int tile = (int)blockIdx.x % a.tiles, which = (int)blockIdx.x / a.tiles;
@@ -560,6 +558,7 @@ static int backward(const LayerNormArgs &a, const T *dy, int64_t lddy, const flo
     int st;
     if (!weights) {  // (the resident workgroups are the faster ones for many rows, also without sums to leave)
         b.part = nullptr;
+        if (dx == nullptr) return OMNI_OK;
         return backward_launch(b, p.fused, 0, p.parts, true, s);
     }
     if (p.fused) {

@@ -143,6 +143,17 @@ template <typename OP> __device__ __forceinline__ float wave_join(float v, OP op
     auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
+// over the lanes whose numbers are equal modulo STRIDE (2, 4 or 8)
+template <int STRIDE, typename OP> __device__ __forceinline__ float join_strided(float v, OP op)
+{
+    if (STRIDE <= 2) v = op(v, dpp<0x4e>(v));   // quad_perm 2 3 0 1
+    if (STRIDE <= 4) v = op(v, dpp<0x124>(v));  // row_ror 4
+    v = op(v, dpp<0x128>(v));                   // row_ror 8
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 
