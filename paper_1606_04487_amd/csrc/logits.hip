@@ -57,6 +57,15 @@ template <typename T> __device__ __forceinline__ void unpack(const uint4 &b, flo
     for (int j = 0; j < CHUNK<T>; ++j) v[j] = u[j];
 }
 
+// Values in the order of whole numbers (-0 counts as 0), with the index below: larger key = larger value, then lower index.
+__device__ __forceinline__ uint32_t ordered(float v)
+{
+    const uint32_t b = __float_as_uint(v + 0.f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float((int32_t)k < 0 ? k & 0x7fffffffu : ~k); }
+constexpr uint32_t ORDERED_NOTHING = 0x007fffffu;  // ordered(-inf)
+
 // ------------------------------------------------------------------------------------------------ running sums
 // Powers of two throughout: e^z = 2^(c (x - m)), c = log2 e / T.  s = sum of them, and in t
 enum Also {
@@ -101,7 +110,8 @@ template <int ALSO> __device__ __forceinline__ void finish(Sums &a, float c)
     a.s *= f;
 }
 
-template <int ALSO, int N> __device__ __forceinline__ void absorb(Sums &a, const float (&x)[N], float c)
+// Takes N elements in; returns their largest.
+template <int ALSO, int N> __device__ __forceinline__ float absorb(Sums &a, const float (&x)[N], float c)
 {
     float g = x[0];
 #pragma unroll
@@ -115,7 +125,7 @@ template <int ALSO, int N> __device__ __forceinline__ void absorb(Sums &a, const
             if (ALSO == Z_TIMES) a.t += fmaxf(z, Z_LEAST) * e;
             if (ALSO >= AT_ONE) a.t += at_one<ALSO>(e, d);
         }
-        return;
+        return g;
     }
     // two chains of sums
     float s1 = 0.f, t1 = 0.f;
@@ -131,6 +141,7 @@ template <int ALSO, int N> __device__ __forceinline__ void absorb(Sums &a, const
     }
     a.s += s1;
     a.t += t1;
+    return g;
 }
 
 template <int ALSO, int BLOCK> __device__ __forceinline__ void join(Sums &a, float c, float *lds)
@@ -144,15 +155,24 @@ template <int ALSO, int BLOCK> __device__ __forceinline__ void join(Sums &a, flo
     finish<ALSO>(a, c);
 }
 
-constexpr int PAIR = 2;  // chunks whose sums are taken together
+constexpr int PAIR = 2, BATCH = 4;  // chunks whose sums are taken together; chunks a thread has in flight
+
+// The largest of every thread's elements by slots of a few batches, in halves of ordered() keys: which chunks of a row can hold
+// one of its largest elements.  Batches of slot i are i << shift and so on.
+constexpr int SLOTS = 16;
+template <int BLOCK> struct Slots {
+    uint16_t most[SLOTS][BLOCK];
+};
 
 // The sums over a row; the thread's own maximum (for the top alternatives) goes to *own.  KEPT chunks a thread, the first ones,
-// are loaded at once and stay in `kept`; the others follow in batches of 4, the next batch in flight while one is summed.
+// are loaded at once and stay in `kept`; the others follow in batches, the next batch in flight while one is summed.  The slots'
+// maxima go to `slots` (null: they are not wanted).
 template <typename T, int BLOCK, int ALSO, bool NT, int KEPT>
-__device__ __forceinline__ Sums row_sums(const T *row, int n, const RowSplit<T> &sp, float c, float *own, float *lds, uint4 (&kept)[KEPT > 0 ? KEPT : 1])
+__device__ __forceinline__ Sums row_sums(const T *row, int n, const RowSplit<T> &sp, float c, float *own, float *lds, uint4 (&kept)[KEPT > 0 ? KEPT : 1],
+                                         Slots<BLOCK> *slots = nullptr, int shift = 0)
 {
-    constexpr int V = CHUNK<T>, BATCH = 4;
-    static_assert(KEPT % PAIR == 0 && BATCH % PAIR == 0, "whole pairs");
+    constexpr int V = CHUNK<T>;
+    static_assert(KEPT % BATCH == 0 && BATCH % PAIR == 0, "whole batches of whole pairs");
     Sums a = {-INFINITY, 0.f, 0.f, 0.f};  // (no maximum yet: h = 0)
     const int tid = threadIdx.x, last = sp.hi - 1;
     auto take = [&](const uint4 *b, int at, bool whole) {  // two chunks; those past the last one, which repeat it, count as -inf
@@ -164,33 +184,39 @@ __device__ __forceinline__ Sums row_sums(const T *row, int n, const RowSplit<T> 
 #pragma unroll
                 for (int j = 0; j < V; ++j) x[u * V + j] = at + u * BLOCK <= last ? x[u * V + j] : -INFINITY;
         }
-        absorb<ALSO>(a, x, c);
+        return absorb<ALSO>(a, x, c);
     };
     auto load = [&](uint4 &b, int at) { b = raw_chunk<T, NT>(row, sp.first(at < last ? at : last)); };
-    int at = sp.lo + tid;
+    int at = sp.lo + tid, first = sp.lo, batch = 0;
+    float most = -INFINITY;
+    auto take_batch = [&](const uint4 *b) {
+        if ((batch & ((1 << shift) - 1)) == 0) most = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < BATCH; u += PAIR)
+            if (first + u * BLOCK < sp.hi) most = fmaxf(most, take(b + u, at + u * BLOCK, first + (u + PAIR) * BLOCK <= sp.hi));
+        if (slots != nullptr) slots->most[batch >> shift][tid] = (uint16_t)(ordered(most) >> 16);
+    };
     if (KEPT > 0 && sp.lo < sp.hi) {
 #pragma unroll
         for (int u = 0; u < KEPT; ++u) load(kept[u], at + u * BLOCK);
 #pragma unroll
-        for (int u = 0; u < KEPT; u += PAIR) {
-            const int first = sp.lo + u * BLOCK;
-            if (first < sp.hi) take(kept + u, at + u * BLOCK, first + PAIR * BLOCK <= sp.hi);
+        for (int u = 0; u < KEPT; u += BATCH) {
+            if (first < sp.hi) take_batch(kept + u);
+            at += BATCH * BLOCK;
+            first += BATCH * BLOCK;
+            ++batch;
         }
     }
-    at += KEPT * BLOCK;
-    int first = sp.lo + KEPT * BLOCK;
     if (first < sp.hi) {
         uint4 b[BATCH], next[BATCH];
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) load(b[u], at + u * BLOCK);
-        for (;;) {
+        for (;; ++batch) {
             const bool more = first + BATCH * BLOCK < sp.hi;
             if (more)
 #pragma unroll
                 for (int u = 0; u < BATCH; ++u) load(next[u], at + (BATCH + u) * BLOCK);
-#pragma unroll
-            for (int u = 0; u < BATCH; u += PAIR)
-                if (first + u * BLOCK < sp.hi) take(b + u, at + u * BLOCK, first + (u + PAIR) * BLOCK <= sp.hi);
+            take_batch(b);
             if (!more) break;
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) b[u] = next[u];
@@ -208,50 +234,70 @@ __device__ __forceinline__ Sums row_sums(const T *row, int n, const RowSplit<T> 
 }
 
 // ------------------------------------------------------------------------------------------------ top alternatives
-// Values in the order of whole numbers (-0 counts as 0), with the index below: larger key = larger value, then lower index.
-__device__ __forceinline__ uint32_t ordered(float v)
-{
-    const uint32_t b = __float_as_uint(v + 0.f);
-    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float((int32_t)k < 0 ? k & 0x7fffffffu : ~k); }
-constexpr uint32_t ORDERED_NOTHING = 0x007fffffu;  // ordered(-inf)
+constexpr int TOP_KEYS = 512, TOP_LIST = 256;
 
-constexpr int TOP_KEYS = 512;
-
-struct TopLds {
+template <int BLOCK> struct TopLds {
     uint64_t keys[TOP_KEYS];
     uint64_t bar;
-    float group[64];
-    int count, threads;
-    uint16_t thread[1024];
+    uint32_t group[256];
+    int count, listed;
+    uint16_t list[TOP_LIST];  // slot * 1024 + thread
 };
 
-// The k largest of a row, k <= 64, in order.  The k-th largest of 64 groups' maxima is a lower bound of the k-th largest
-// element; the elements that reach it are collected (few more than k) and ranked by comparing each with all.  Only threads whose
-// own maximum reaches the bound can hold one, so only those threads' chunks are read a second time, one such thread's chunks by
-// all lanes of a wavefront.  When more elements reach the bound than there is room for (equal or oddly placed values), the k-th
-// largest of those collected is a higher bound, and the collection is done again: every key is different, so this ends.
-template <typename T, int BLOCK>
-__device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &sp, float own, int k, float m, float inv_t, float lns, int64_t *index, float *lp, TopLds &t)
+// The k largest of a row, k <= 64, in order.  The k-th largest of the maxima of 256 groups of threads (of single chunks, in a
+// workgroup of one wavefront) is a lower bound of the k-th largest element; the elements that reach it are collected, few more
+// than k, and ranked by comparing each with all.  A row that the threads keep (KEPT > 0) is looked through where it lies; of others
+// only the slots whose maximum reaches the bound are read again, their chunks spread over the workgroup (every chunk of the
+// threads that reach it instead: 149 us for 32 of 2048 x 131072 bf16, where the sums alone take 85: the chunks of one thread lie
+// in as many cache lines, and half of the row came a second time).  When more elements reach the bound than there is room for
+// (equal values), the k-th largest of those collected is a higher bound, and the collection is done again: every key is
+// different, so this ends.
+template <typename T, int BLOCK, int KEPT>
+__device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &sp, float own, int k, float m, float inv_t, float lns, int64_t *index, float *lp,
+                                        TopLds<BLOCK> &t, const uint4 (&kept)[KEPT > 0 ? KEPT : 1], const Slots<BLOCK> *slots, int shift)
 {
-    constexpr int V = CHUNK<T>, WAVES = BLOCK / 64;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
-    // groups of WAVES threads of one wavefront each: 64 / WAVES groups a wavefront
-    float g = own;
+    constexpr int V = CHUNK<T>, EACH = BLOCK == 64 ? KEPT : 4;  // groups that a lane compares
+    const int tid = threadIdx.x, lane = tid & 63, rest = KEPT > 0 ? sp.hi : sp.lo;
+    uint32_t u[EACH], bound = 0;
+    if constexpr (BLOCK == 64) {  // every chunk is a group
 #pragma unroll
-    for (int off = 1; off < WAVES; off *= 2) g = fmaxf(g, __shfl_xor(g, off, 64));
-    if (tid == 0) t.threads = 0;
-    if (lane % WAVES == 0) t.group[wave * (64 / WAVES) + lane / WAVES] = g;
-    __syncthreads();
-    const uint32_t u = ordered(t.group[lane]);
-    uint32_t bound = 0;
+        for (int i = 0; i < EACH; ++i) {
+            float x[V], g = i == 0 && tid < sp.edges ? element(row + sp.edge(tid, n)) : -INFINITY;
+            unpack<T>(kept[i], x);
+#pragma unroll
+            for (int j = 0; j < V; ++j) g = sp.lo + tid + i * 64 < sp.hi ? fmaxf(g, x[j]) : g;
+            u[i] = ordered(fmaxf(g, -INFINITY));
+        }
+    } else {
+        float g = own;
+        if (BLOCK == 1024) {
+            g = fmaxf(g, dpp<0xb1>(g));
+            g = fmaxf(g, dpp<0x4e>(g));
+        }
+        if (tid % (BLOCK / 256) == 0) t.group[tid / (BLOCK / 256)] = ordered(g);
+        if (tid == 0) t.listed = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) u[i] = t.group[i * 64 + lane];
+    }
     for (int bit = 31; bit >= 0; --bit) {
         const uint32_t more = bound | (1u << bit);
-        if (__popcll(__ballot(u >= more)) >= k) bound = more;
+        int reach = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) reach += __popcll(__ballot(u[i] >= more));
+        if (reach >= k) bound = more;
+        if (reach == k) break;
     }
     if (bound <= ORDERED_NOTHING) bound = ORDERED_NOTHING + 1;  // -inf is nobody's alternative
-    if (ordered(own) >= bound && own > -INFINITY) t.thread[atomicAdd(&t.threads, 1)] = (uint16_t)tid;
+    const bool able = ordered(own) >= bound;
+    // slots that reach the bound; past the list's room, every chunk is looked through
+    const int batches = rest < sp.hi ? (sp.hi - rest + BATCH * BLOCK - 1) / (BATCH * BLOCK) : 0;
+    if (able)
+        for (int i = 0; i << shift < batches; ++i)
+            if (slots->most[i][tid] >= bound >> 16) {
+                const int to = atomicAdd(&t.listed, 1);
+                if (to < TOP_LIST) t.list[to] = (uint16_t)(i * 1024 + tid);
+            }
     uint64_t bar = (uint64_t)bound << 32;
     int found;
     for (;;) {
@@ -265,15 +311,27 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
                 if (to < TOP_KEYS) t.keys[to] = key;
             }
         };
-        for (int a = wave; a < t.threads; a += WAVES) {
-            const int who = t.thread[a];
-            for (int c = sp.lo + who + lane * BLOCK; c < sp.hi; c += 64 * BLOCK) {
-                float x[V];
-                unpack<T>(raw_chunk<T, false>(row, sp.first(c)), x);
+        auto offer_chunk = [&](const uint4 &b, int c) {
+            float x[V];
+            unpack<T>(b, x);
 #pragma unroll
-                for (int j = 0; j < V; ++j) offer(x[j], sp.first(c) + j);
+            for (int j = 0; j < V; ++j) offer(x[j], sp.first(c) + j);
+        };
+        if (able) {
+#pragma unroll
+            for (int i = 0; i < KEPT; ++i)
+                if (sp.lo + tid + i * BLOCK < sp.hi && (BLOCK != 64 || u[i] >= bound)) offer_chunk(kept[i], sp.lo + tid + i * BLOCK);
+            if (tid < sp.edges) offer(element(row + sp.edge(tid, n)), sp.edge(tid, n));
+        }
+        const int listed = KEPT > 0 ? 0 : t.listed;
+        if (listed <= TOP_LIST) {
+            const int each = 2 + shift;  // chunks of a slot: BATCH << shift
+            for (int i = tid; i < listed << each; i += BLOCK) {
+                const int e = t.list[i >> each], q = i & ((1 << each) - 1), c = rest + (e & 1023) + (((e >> 10) << each) + q) * BLOCK;
+                if (c < sp.hi) offer_chunk(raw_chunk<T, false>(row, sp.first(c)), c);
             }
-            if (lane == 0 && who < sp.edges) offer(element(row + sp.edge(who, n)), sp.edge(who, n));
+        } else {
+            for (int c = rest + tid; c < sp.hi; c += BLOCK) offer_chunk(raw_chunk<T, false>(row, sp.first(c)), c);
         }
         __syncthreads();
         found = t.count;
@@ -302,20 +360,23 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
 }
 
 // ------------------------------------------------------------------------------------------------ log probabilities
-template <typename T, int BLOCK, bool ENTROPY>
-__global__ __launch_bounds__(BLOCK) void logprob_forward_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int n, float c, float inv_t,
+template <typename T, int BLOCK, int KEPT, bool ENTROPY>
+__global__ __launch_bounds__(BLOCK) void logprob_forward_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int n, float c, float inv_t, int shift,
                                                                 const int64_t *__restrict__ targets, int given, float *__restrict__ logprob, float *__restrict__ entropy,
                                                                 int top, int64_t *__restrict__ top_index, float *__restrict__ top_logprob, float *__restrict__ stats)
 {
     __shared__ float lds[2 * (BLOCK / 64)];
-    __shared__ TopLds tl;
+    __shared__ TopLds<BLOCK> tl;
+    constexpr bool WHOLE = KEPT > 0 && BLOCK < 1024;  // this variant is launched for rows that it keeps whole
+    __shared__ Slots<WHOLE ? 1 : BLOCK> sl;
+    Slots<BLOCK> *slots = WHOLE || top == 0 ? nullptr : reinterpret_cast<Slots<BLOCK> *>(&sl);
     const int64_t r = grid_row();
     if (r >= rows) return;
     const T *row = logits + r * ld;
     const RowSplit<T> sp(row, n);
     float own;
-    uint4 none[1];
-    const Sums a = row_sums<T, BLOCK, ENTROPY ? Z_TIMES : NOTHING, true, 0>(row, n, sp, c, &own, lds, none);
+    uint4 kept[KEPT > 0 ? KEPT : 1];
+    const Sums a = row_sums<T, BLOCK, ENTROPY ? Z_TIMES : NOTHING, true, KEPT>(row, n, sp, c, &own, lds, kept, slots, shift);
     const float lns = logf(a.s);
     if (threadIdx.x == 0) {
         if (ENTROPY) entropy[r] = a.m == -INFINITY && a.s == 0.f ? 0.f : lns - LN2 * a.t / a.s;
@@ -327,7 +388,14 @@ __global__ __launch_bounds__(BLOCK) void logprob_forward_kernel(const T *__restr
         if (at >= 0 && at < n) v = a.m == -INFINITY && a.s == 0.f ? -INFINITY : (element(row + at) - a.m) * inv_t - lns;
         logprob[r * given + i] = v;
     }
-    if (top > 0) row_top<T, BLOCK>(row, n, sp, own, top, a.m, inv_t, lns, top_index + r * top, top_logprob + r * top, tl);
+    if (top > 0) {
+        if constexpr (WHOLE) {
+            row_top<T, BLOCK, KEPT>(row, n, sp, own, top, a.m, inv_t, lns, top_index + r * top, top_logprob + r * top, tl, kept, slots, shift);
+        } else {
+            uint4 none[1];
+            row_top<T, BLOCK, 0>(row, n, sp, own, top, a.m, inv_t, lns, top_index + r * top, top_logprob + r * top, tl, none, slots, shift);
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ gradients
@@ -481,24 +549,38 @@ static int row_block(const LogitsArgs &a)
         }                                           \
     } while (0)
 
+template <typename T> static int logprob_forward(const LogitsArgs &a, const int64_t *targets, int given, float *logprob, float *entropy, int top, int64_t *top_index,
+                                                float *top_logprob, float *stats, hipStream_t s)
+{
+    const int64_t chunks = a.classes / CHUNK<T>;
+    const float inv_t = 1.f / a.temperature, c = LOG2E / a.temperature;
+#define OMNI_LOGPROB(B, K)                                                                                                                                                    \
+    do {                                                                                                                                                                      \
+        int shift = 0; /* at most SLOTS slots; one chunk more than the row has, since chunks begin at an aligned address */                                                    \
+        while (((chunks / (BATCH * B)) >> shift) + 1 > SLOTS) ++shift;                                                                                                         \
+        if (entropy != nullptr)                                                                                                                                               \
+            hipLaunchKernelGGL((logprob_forward_kernel<T, B, K, true>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, c, inv_t, shift, targets, \
+                               given, logprob, entropy, top, top_index, top_logprob, stats);                                                                                  \
+        else                                                                                                                                                                  \
+            hipLaunchKernelGGL((logprob_forward_kernel<T, B, K, false>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, c, inv_t, shift, targets, \
+                               given, logprob, entropy, top, top_index, top_logprob, stats);                                                                                  \
+    } while (0)
+    if (chunks <= 256) OMNI_LOGPROB(64, 4);
+    else if (chunks <= 512) OMNI_LOGPROB(64, 8);
+    else if (chunks <= 1024) OMNI_LOGPROB(256, 4);
+    else if (a.rows < 512) OMNI_LOGPROB(1024, 16);
+    else OMNI_LOGPROB(256, 0);
+#undef OMNI_LOGPROB
+    OMNI_LAUNCH_CHECK();
+    return OMNI_OK;
+}
+
 int launch_logprob_forward(const LogitsArgs &a, const int64_t *targets, int given, float *logprob, float *entropy, int top, int64_t *top_index, float *top_logprob,
                            float *stats, hipStream_t s)
 {
     ProfScope prof(KID_LOGPROB, s, 0.0, (double)a.rows * a.classes * elem_size(a.dtype));
-    const float inv_t = 1.f / a.temperature, c = LOG2E / a.temperature;
-#define OMNI_LOGPROB(T, B)                                                                                                                                          \
-    do {                                                                                                                                                            \
-        if (entropy != nullptr)                                                                                                                                     \
-            hipLaunchKernelGGL((logprob_forward_kernel<T, B, true>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, c, inv_t, targets, \
-                               given, logprob, entropy, top, top_index, top_logprob, stats);                                                                        \
-        else                                                                                                                                                        \
-            hipLaunchKernelGGL((logprob_forward_kernel<T, B, false>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, c, inv_t, targets, \
-                               given, logprob, entropy, top, top_index, top_logprob, stats);                                                                        \
-    } while (0)
-    OMNI_BY_TYPE_AND_BLOCK(OMNI_LOGPROB);
-#undef OMNI_LOGPROB
-    OMNI_LAUNCH_CHECK();
-    return OMNI_OK;
+    return a.dtype == OMNI_BF16 ? logprob_forward<bf16_t>(a, targets, given, logprob, entropy, top, top_index, top_logprob, stats, s)
+                                : logprob_forward<float>(a, targets, given, logprob, entropy, top, top_index, top_logprob, stats, s);
 }
 
 // ------------------------------------------------------------------------------------------------ distillation
