@@ -352,8 +352,7 @@ int omni_dropout_backward(int32_t dtype, int64_t count, float p, uint64_t seed, 
  *       receive mu and r; the backward pass needs them.  y may be x.
  *   layer_norm_backward: with xh = (x - mu) r, g = dy gamma:  dx = r (g - mean g - xh mean(g xh)),
  *       dgamma = sum over rows of dy xh, dbeta = sum over rows of dy (fp32 [width], in an order that only the sizes decide).
- *       dx, dgamma and dbeta are nullable, not all three.  workspace as omni_layer_norm_workspace_bytes says (host only; 0: it may
- *       be NULL); without dgamma and dbeta none is needed.  dx may be x or dy.
+ *       dx, dgamma and dbeta are nullable, not all three.  Without dgamma and dbeta no workspace is needed.  dx may be x or dy.
  *
  *   logprob_forward : ln p = z - ln sum exp z, z = (logits - max) / temperature, of a row's classes (at most 2^30).
  *       logprob [rows][given] receives ln p of the classes targets [rows][given] (given <= 1024; 0: none).  A target below 0
@@ -381,6 +380,7 @@ int omni_dropout_backward(int32_t dtype, int64_t count, float p, uint64_t seed, 
  *       w = scale * dloss[row] (dloss fp32 [rows], nullable: 1), without the terms that the loss is without.  dlogits may be
  *       logits.
  *   distill_forward_backward: both, reading a row once from memory.  dlogits may be logits.
+ * Workspaces as the *_workspace_bytes calls say (host only; 0: NULL will do): few long rows are worked on in parts.
  */
 int omni_layer_norm_forward(int32_t dtype, int64_t rows, int64_t width, const void *x, int64_t ldx, const float *gamma,
                             const float *beta, float eps, void *y, int64_t ldy, float *mean, float *rstd, void *hip_stream);
@@ -388,22 +388,24 @@ int omni_layer_norm_workspace_bytes(int32_t dtype, int64_t rows, int64_t width, 
 int omni_layer_norm_backward(int32_t dtype, int64_t rows, int64_t width, const void *x, int64_t ldx, const void *dy, int64_t lddy,
                              const float *gamma, const float *mean, const float *rstd, void *dx, int64_t lddx, float *dgamma,
                              float *dbeta, void *workspace, size_t workspace_bytes, void *hip_stream);
+int omni_logprob_workspace_bytes(int32_t dtype, int64_t rows, int64_t classes, int32_t top, size_t *bytes);
 int omni_logprob_forward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, float temperature,
                          const int64_t *targets, int32_t given, float *logprob, float *entropy, int32_t top, int64_t *top_index,
-                         float *top_logprob, float *stats, void *hip_stream);
+                         float *top_logprob, float *stats, void *workspace, size_t workspace_bytes, void *hip_stream);
 int omni_logprob_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, float temperature,
                           const float *stats, const int64_t *targets, int32_t given, const float *dlogprob, const float *dentropy,
                           const float *entropy, void *dlogits, int64_t ld_out, void *hip_stream);
+int omni_distill_workspace_bytes(int32_t dtype, int64_t rows, int64_t classes, size_t *bytes);
 int omni_distill_forward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const int64_t *teacher_index,
                          const float *teacher_logits, int32_t kept, const int64_t *labels, float temperature, float alpha,
-                         float *loss, float *stats, void *hip_stream);
+                         float *loss, float *stats, void *workspace, size_t workspace_bytes, void *hip_stream);
 int omni_distill_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const int64_t *teacher_index,
                           const float *teacher_logits, int32_t kept, const int64_t *labels, float temperature, float alpha,
                           const float *stats, const float *dloss, float scale, void *dlogits, int64_t ld_out, void *hip_stream);
 int omni_distill_forward_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld,
                                   const int64_t *teacher_index, const float *teacher_logits, int32_t kept, const int64_t *labels,
                                   float temperature, float alpha, const float *dloss, float scale, float *loss, void *dlogits,
-                                  int64_t ld_out, void *hip_stream);
+                                  int64_t ld_out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Per-kernel timing (the paper times with a wall clock, App. C "Experiment Setup"; on a GPU the

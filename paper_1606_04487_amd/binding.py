@@ -37,8 +37,8 @@ SYMBOLS = [
     "omni_conv_dy_rows_layout", "omni_relu_backward_rows", "omni_maxpool_backward_rows", "omni_conv_backward_weights_rows",
     "omni_conv_backward_data_rows", "omni_conv_backward_data_relu_rows_sums", "omni_conv_backward_data_relu_rows",
     "omni_lrn_forward", "omni_lrn_backward", "omni_dropout_forward", "omni_dropout_backward",
-    "omni_layer_norm_forward", "omni_layer_norm_workspace_bytes", "omni_layer_norm_backward", 
-    "omni_logprob_forward", "omni_logprob_backward", "omni_distill_forward", "omni_distill_backward",
+    "omni_layer_norm_forward", "omni_layer_norm_workspace_bytes", "omni_layer_norm_backward", "omni_logprob_workspace_bytes",
+    "omni_logprob_forward", "omni_logprob_backward", "omni_distill_workspace_bytes", "omni_distill_forward", "omni_distill_backward",
     "omni_distill_forward_backward", "omni_status_string", "omni_version", "omni_tuning_set",
     "omni_profile_enable", "omni_profile_select", "omni_profile_select_mask", "omni_profile_kernel_count", "omni_profile_kernel_name", "omni_profile_summary",
 ]
@@ -106,11 +106,13 @@ _lib.omni_dropout_backward.argtypes = [_i32, _i64, _f, _u64, _u64, _vp, _vp, _vp
 _lib.omni_layer_norm_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _f, _vp, _i64, _vp, _vp, _vp]
 _lib.omni_layer_norm_workspace_bytes.argtypes = [_i32, _i64, _i64, ctypes.POINTER(_sz)]
 _lib.omni_layer_norm_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _sz, _vp]
-_lib.omni_logprob_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _f, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp]
+_lib.omni_logprob_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _f, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.omni_logprob_workspace_bytes.argtypes = [_i32, _i64, _i64, _i32, ctypes.POINTER(_sz)]
 _lib.omni_logprob_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _f, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _i64, _vp]
-_lib.omni_distill_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _vp, _vp]
+_lib.omni_distill_workspace_bytes.argtypes = [_i32, _i64, _i64, ctypes.POINTER(_sz)]
+_lib.omni_distill_forward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _vp, _vp, _sz, _vp]
 _lib.omni_distill_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _vp, _f, _vp, _i64, _vp]
-_lib.omni_distill_forward_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _f, _vp, _vp, _i64, _vp]
+_lib.omni_distill_forward_backward.argtypes = [_i32, _i64, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _f, _f, _vp, _f, _vp, _vp, _i64, _vp, _sz, _vp]
 
 _lib.omni_profile_enable.argtypes = [ctypes.c_int]
 _lib.omni_profile_select_mask.argtypes = [ctypes.c_uint64]
@@ -627,6 +629,34 @@ def layer_norm_workspace_bytes(rows: int, width: int, dtype: torch.dtype = torch
     return b.value
 
 
+@functools.lru_cache(maxsize=1024)
+def logprob_workspace_bytes(rows: int, classes: int, top: int = 0, dtype: torch.dtype = torch.float32) -> int:
+    """omni_logprob_workspace_bytes: scratch of logprob_forward (0: none)."""
+    b = _sz()
+    _check(_lib.omni_logprob_workspace_bytes(dtype_code(dtype), rows, classes, top, ctypes.byref(b)))
+    return b.value
+
+
+@functools.lru_cache(maxsize=1024)
+def distill_workspace_bytes(rows: int, classes: int, dtype: torch.dtype = torch.float32) -> int:
+    """omni_distill_workspace_bytes: scratch of distill_forward and distill_forward_backward (0: none)."""
+    b = _sz()
+    _check(_lib.omni_distill_workspace_bytes(dtype_code(dtype), rows, classes, ctypes.byref(b)))
+    return b.value
+
+
+def _scratch(need: int, workspace: Optional[torch.Tensor], dev: int, device):
+    """(pointer, bytes, tensor) of the caller's workspace, or else of one from torch's allocator, which keeps its memory for the
+    work queued on this stream."""
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace.data_ptr(), need, workspace
+    n = workspace.numel()
+    return _vector(workspace, n, workspace.dtype, dev, "workspace"), n * workspace.element_size(), workspace
+
+
 def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, y=None, mean=None, rstd=None, want_stats: bool = True):
     """omni_layer_norm_forward over x's last axis; returns (y, mean, rstd) -- mean and rstd (fp32, one a row) are what
     layer_norm_backward needs (None without want_stats, unless they are given)."""
@@ -648,8 +678,7 @@ def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, y=None, mean
 
 def layer_norm_backward(x, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, want_dx: bool = True,
                         want_dweights: bool = True, workspace=None):
-    """omni_layer_norm_backward; returns (dx, dgamma, dbeta), dgamma and dbeta fp32 [width].  Without a workspace one is taken
-    from torch's allocator, which keeps its memory for the work queued on this stream."""
+    """omni_layer_norm_backward; returns (dx, dgamma, dbeta), dgamma and dbeta fp32 [width]."""
     dev, dtype = _device(x, "x"), x.dtype
     px, rows, width, ldx = _matrix(x, dev, "x")
     pdy, lddy = _like(dy, rows, width, dtype, dev, "dy")
@@ -661,14 +690,8 @@ def layer_norm_backward(x, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbe
             dgamma = torch.empty((width,), dtype=_f32, device=x.device)
         if dbeta is None:
             dbeta = torch.empty((width,), dtype=_f32, device=x.device)
-    if workspace is None and (dgamma is not None or dbeta is not None):
-        need = layer_norm_workspace_bytes(rows, width, dtype)
-        if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-    pw, nw = None, 0
-    if workspace is not None:
-        nw = workspace.numel() * workspace.element_size()
-        pw = _vector(workspace, workspace.numel(), workspace.dtype, dev, "workspace")
+    weights = dgamma is not None or dbeta is not None
+    pw, nw, workspace = _scratch(layer_norm_workspace_bytes(rows, width, dtype) if weights else 0, workspace, dev, x.device)
     _check(_lib.omni_layer_norm_backward(dtype_code(dtype), rows, width, px, ldx, pdy, lddy, _vector(gamma, width, _f32, dev, "gamma"),
                                          _vector(mean, rows, _f32, dev, "mean"), _vector(rstd, rows, _f32, dev, "rstd"), pdx, lddx,
                                          _vector(dgamma, width, _f32, dev, "dgamma"), _vector(dbeta, width, _f32, dev, "dbeta"), pw, nw,
@@ -687,7 +710,7 @@ def _per_row(t: Optional[torch.Tensor], rows: int, what: str) -> int:
 
 
 def logprob_forward(logits, targets=None, top: int = 0, temperature: float = 1.0, logprob=None, entropy=None, top_index=None,
-                    top_logprob=None, stats=None, want_entropy: bool = True, want_stats: bool = True):
+                    top_logprob=None, stats=None, want_entropy: bool = True, want_stats: bool = True, workspace=None):
     """omni_logprob_forward over logits [..., classes]; returns (logprob, entropy, top_index, top_logprob, stats).  targets:
     int64, any number of classes a row; logprob has targets' shape, entropy one value a row, top_index (int64) and top_logprob
     `top` a row; stats is what logprob_backward needs.  What is not asked for is None."""
@@ -705,12 +728,13 @@ def logprob_forward(logits, targets=None, top: int = 0, temperature: float = 1.0
             top_logprob = torch.empty(logits.shape[:-1] + (top,), dtype=_f32, device=logits.device)
     if stats is None and want_stats:
         stats = torch.empty(logits.shape[:-1] + (2,), dtype=_f32, device=logits.device)
+    pw, nw, workspace = _scratch(logprob_workspace_bytes(rows, classes, top, logits.dtype), workspace, dev, logits.device)
     _check(_lib.omni_logprob_forward(dtype_code(logits.dtype), rows, classes, p, ld, temperature,
                                      _vector(targets, rows * given, _int64, dev, "targets"), given,
                                      _vector(logprob, rows * given, _f32, dev, "logprob"), _vector(entropy, rows, _f32, dev, "entropy"), top,
                                      _vector(top_index, rows * top, _int64, dev, "top_index"),
                                      _vector(top_logprob, rows * top, _f32, dev, "top_logprob"),
-                                     _vector(stats, 2 * rows, _f32, dev, "stats"), _stream_of(dev)))
+                                     _vector(stats, 2 * rows, _f32, dev, "stats"), pw, nw, _stream_of(dev)))
     return logprob, entropy, top_index, top_logprob, stats
 
 
@@ -740,7 +764,7 @@ def _teacher(index, values, labels, rows: int, dev: int):
 
 
 def distill_forward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0, loss=None,
-                    stats=None, want_stats: bool = True):
+                    stats=None, want_stats: bool = True, workspace=None):
     """omni_distill_forward over logits [..., classes]; returns (loss, stats): the loss of every row, and what distill_backward
     needs.  Without teacher entries (and alpha = 0) it is the labels' cross entropy."""
     dev = _device(logits, "logits")
@@ -750,8 +774,10 @@ def distill_forward(logits, teacher_index=None, teacher_logits=None, labels=None
         loss = torch.empty(logits.shape[:-1], dtype=_f32, device=logits.device)
     if stats is None and want_stats:
         stats = torch.empty(logits.shape[:-1] + (4,), dtype=_f32, device=logits.device)
+    pw, nw, workspace = _scratch(distill_workspace_bytes(rows, classes, logits.dtype), workspace, dev, logits.device)
     _check(_lib.omni_distill_forward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                     _vector(loss, rows, _f32, dev, "loss"), _vector(stats, 4 * rows, _f32, dev, "stats"), _stream_of(dev)))
+                                     _vector(loss, rows, _f32, dev, "loss"), _vector(stats, 4 * rows, _f32, dev, "stats"), pw, nw,
+                                     _stream_of(dev)))
     return loss, stats
 
 
@@ -771,7 +797,7 @@ def distill_backward(logits, teacher_index=None, teacher_logits=None, labels=Non
 
 
 def distill_forward_backward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0,
-                             dloss=None, scale: float = 1.0, loss=None, dlogits=None):
+                             dloss=None, scale: float = 1.0, loss=None, dlogits=None, workspace=None):
     """omni_distill_forward_backward: distill_forward and distill_backward in one call; returns (loss, dlogits)."""
     dev, dtype = _device(logits, "logits"), logits.dtype
     p, rows, classes, ld = _matrix(logits, dev, "logits")
@@ -781,9 +807,10 @@ def distill_forward_backward(logits, teacher_index=None, teacher_logits=None, la
     if dlogits is None:
         dlogits = torch.empty(logits.shape, dtype=dtype, device=logits.device)
     po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits")
+    pw, nw, workspace = _scratch(distill_workspace_bytes(rows, classes, dtype), workspace, dev, logits.device)
     _check(_lib.omni_distill_forward_backward(dtype_code(dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
                                               _vector(dloss, rows, _f32, dev, "dloss"), scale, _vector(loss, rows, _f32, dev, "loss"), po, ldo,
-                                              _stream_of(dev)))
+                                              pw, nw, _stream_of(dev)))
     return loss, dlogits
 
 

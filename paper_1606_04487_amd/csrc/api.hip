@@ -1020,6 +1020,12 @@ static bool all_aligned16(std::initializer_list<const void *> ps)
     return true;
 }
 
+static int check_workspace(const void *workspace, size_t workspace_bytes, size_t need)
+{
+    if (need > 0 && workspace == nullptr) return OMNI_INVALID_ARGUMENT;
+    return workspace_bytes < need ? OMNI_WORKSPACE_TOO_SMALL : OMNI_OK;
+}
+
 static const int64_t NORM_WIDEST = 1 << 28, MOST_CLASSES = 1 << 30;
 
 int omni_layer_norm_forward(int32_t dtype, int64_t rows, int64_t width, const void *x, int64_t ldx, const float *gamma, const float *beta, float eps,
@@ -1057,9 +1063,7 @@ int omni_layer_norm_backward(int32_t dtype, int64_t rows, int64_t width, const v
     if (dx != nullptr && (!may_share(dx, lddx, x, ldx) || !may_share(dx, lddx, dy, lddy))) return OMNI_INVALID_ARGUMENT;
     if (!all_aligned16({x, dy, gamma, mean, rstd, dx, dgamma, dbeta, workspace})) return OMNI_MISALIGNED;
     if (dgamma != nullptr || dbeta != nullptr) {
-        const size_t need = layer_norm_workspace(dtype, rows, width);
-        if (need > 0 && workspace == nullptr) return OMNI_INVALID_ARGUMENT;
-        if (workspace_bytes < need) return OMNI_WORKSPACE_TOO_SMALL;
+        if ((st = check_workspace(workspace, workspace_bytes, layer_norm_workspace(dtype, rows, width))) != OMNI_OK) return st;
     }
     return launch_layer_norm_backward(LayerNormArgs{dtype, rows, width, x, ldx, gamma}, dy, lddy, mean, rstd, rows > 0 ? dx : nullptr, lddx, dgamma, dbeta,
                                       (float *)workspace, (hipStream_t)hip_stream);
@@ -1074,9 +1078,19 @@ static int check_logits(int32_t dtype, int64_t rows, int64_t classes, int64_t ld
     return check_pitch(rows, classes, ld);
 }
 
+int omni_logprob_workspace_bytes(int32_t dtype, int64_t rows, int64_t classes, int32_t top, size_t *bytes)
+{
+    if (bytes == nullptr || top < 0) return OMNI_INVALID_ARGUMENT;
+    int st = check_rows(dtype, rows, classes, MOST_CLASSES);
+    if (st != OMNI_OK) return st;
+    if (top > TOP_MOST) return OMNI_UNSUPPORTED;
+    *bytes = logprob_workspace(dtype, rows, classes, top);
+    return OMNI_OK;
+}
+
 int omni_logprob_forward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, float temperature, const int64_t *targets,
                          int32_t given, float *logprob, float *entropy, int32_t top, int64_t *top_index, float *top_logprob, float *stats,
-                         void *hip_stream)
+                         void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     int st = check_logits(dtype, rows, classes, ld, temperature);
     if (st != OMNI_OK) return st;
@@ -1085,9 +1099,10 @@ int omni_logprob_forward(int32_t dtype, int64_t rows, int64_t classes, const voi
     if (rows == 0) return OMNI_OK;
     if (logits == nullptr || (given > 0 && (targets == nullptr || logprob == nullptr)) || (top > 0 && (top_index == nullptr || top_logprob == nullptr)))
         return OMNI_INVALID_ARGUMENT;
-    if (!all_aligned16({logits, targets, logprob, entropy, top_index, top_logprob, stats})) return OMNI_MISALIGNED;
+    if (!all_aligned16({logits, targets, logprob, entropy, top_index, top_logprob, stats, workspace})) return OMNI_MISALIGNED;
+    if ((st = check_workspace(workspace, workspace_bytes, logprob_workspace(dtype, rows, classes, top))) != OMNI_OK) return st;
     return launch_logprob_forward(LogitsArgs{dtype, rows, classes, logits, ld, temperature}, targets, given, logprob, entropy, top, top_index, top_logprob,
-                                  stats, (hipStream_t)hip_stream);
+                                  stats, workspace, (hipStream_t)hip_stream);
 }
 
 int omni_logprob_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, float temperature, const float *stats,
@@ -1125,27 +1140,39 @@ static int make_distill(int32_t dtype, int64_t rows, int64_t classes, int64_t ld
     return OMNI_OK;
 }
 
+int omni_distill_workspace_bytes(int32_t dtype, int64_t rows, int64_t classes, size_t *bytes)
+{
+    if (bytes == nullptr) return OMNI_INVALID_ARGUMENT;
+    int st = check_rows(dtype, rows, classes, MOST_CLASSES);
+    if (st != OMNI_OK) return st;
+    *bytes = distill_workspace(dtype, rows, classes);
+    return OMNI_OK;
+}
+
 int omni_distill_forward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const int64_t *teacher_index, const float *teacher_logits,
-                         int32_t kept, const int64_t *labels, float temperature, float alpha, float *loss, float *stats, void *hip_stream)
+                         int32_t kept, const int64_t *labels, float temperature, float alpha, float *loss, float *stats, void *workspace,
+                         size_t workspace_bytes, void *hip_stream)
 {
     DistillArgs d;
     int st = make_distill(dtype, rows, classes, ld, logits, teacher_index, teacher_logits, kept, labels, temperature, alpha, nullptr, 1.f, &d);
     if (st != OMNI_OK || rows == 0) return st;
     if (loss == nullptr) return OMNI_INVALID_ARGUMENT;
-    if (!all_aligned16({loss, stats})) return OMNI_MISALIGNED;
-    return launch_distill_loss(LogitsArgs{dtype, rows, classes, logits, ld, temperature}, d, loss, stats, (hipStream_t)hip_stream);
+    if (!all_aligned16({loss, stats, workspace})) return OMNI_MISALIGNED;
+    if ((st = check_workspace(workspace, workspace_bytes, distill_workspace(dtype, rows, classes))) != OMNI_OK) return st;
+    return launch_distill_loss(LogitsArgs{dtype, rows, classes, logits, ld, temperature}, d, loss, stats, workspace, (hipStream_t)hip_stream);
 }
 
 int omni_distill_forward_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const int64_t *teacher_index,
                                   const float *teacher_logits, int32_t kept, const int64_t *labels, float temperature, float alpha, const float *dloss,
-                                  float scale, float *loss, void *dlogits, int64_t ld_out, void *hip_stream)
+                                  float scale, float *loss, void *dlogits, int64_t ld_out, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     DistillArgs d;
     int st = make_distill(dtype, rows, classes, ld, logits, teacher_index, teacher_logits, kept, labels, temperature, alpha, dloss, scale, &d);
     if (st != OMNI_OK || (st = check_pitch(rows, classes, ld_out)) != OMNI_OK || rows == 0) return st;
     if (loss == nullptr || dlogits == nullptr || !may_share(dlogits, ld_out, logits, ld)) return OMNI_INVALID_ARGUMENT;
-    if (!all_aligned16({loss, dlogits})) return OMNI_MISALIGNED;
-    return launch_distill_both(LogitsArgs{dtype, rows, classes, logits, ld, temperature}, d, loss, dlogits, ld_out, (hipStream_t)hip_stream);
+    if (!all_aligned16({loss, dlogits, workspace})) return OMNI_MISALIGNED;
+    if ((st = check_workspace(workspace, workspace_bytes, distill_workspace(dtype, rows, classes))) != OMNI_OK) return st;
+    return launch_distill_both(LogitsArgs{dtype, rows, classes, logits, ld, temperature}, d, loss, dlogits, ld_out, workspace, (hipStream_t)hip_stream);
 }
 
 int omni_distill_backward(int32_t dtype, int64_t rows, int64_t classes, const void *logits, int64_t ld, const int64_t *teacher_index, const float *teacher_logits,

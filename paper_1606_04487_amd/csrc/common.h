@@ -317,13 +317,15 @@ int launch_layer_norm_backward(const LayerNormArgs &a, const void *dy, int64_t l
 // logits.hip: rows of logits [rows][ld], `classes` elements each
 constexpr int TOP_MOST = 64, GIVEN_MOST = 1024, KEPT_MOST = 256;  // top alternatives, given classes, teacher's entries of a row
 struct LogitsArgs { int dtype; int64_t rows, classes; const void *logits; int64_t ld; float temperature; };
+size_t logprob_workspace(int dtype, int64_t rows, int64_t classes, int top);
+size_t distill_workspace(int dtype, int64_t rows, int64_t classes);
 int launch_logprob_forward(const LogitsArgs &a, const int64_t *targets, int given, float *logprob, float *entropy, int top, int64_t *top_index,
-                           float *top_logprob, float *stats, hipStream_t s);
+                           float *top_logprob, float *stats, void *workspace, hipStream_t s);
 int launch_logprob_backward(const LogitsArgs &a, const int64_t *targets, int given, const float *dlogprob, const float *dentropy, const float *entropy,
                             const float *stats, void *out, int64_t ld_out, hipStream_t s);
 struct DistillArgs { const int64_t *index; const float *teacher; int kept; const int64_t *labels; float temperature, alpha; const float *dloss; float scale; };
-int launch_distill_loss(const LogitsArgs &a, const DistillArgs &d, float *loss, float *stats, hipStream_t s);
-int launch_distill_both(const LogitsArgs &a, const DistillArgs &d, float *loss, void *out, int64_t ld_out, hipStream_t s);
+int launch_distill_loss(const LogitsArgs &a, const DistillArgs &d, float *loss, float *stats, void *workspace, hipStream_t s);
+int launch_distill_both(const LogitsArgs &a, const DistillArgs &d, float *loss, void *out, int64_t ld_out, void *workspace, hipStream_t s);
 int launch_distill_backward(const LogitsArgs &a, const DistillArgs &d, const float *stats, void *out, int64_t ld_out, hipStream_t s);
 
 }  // namespace omni

@@ -252,14 +252,18 @@ template <int BLOCK> struct TopLds {
 // in as many cache lines, and half of the row came a second time).  When more elements reach the bound than there is room for
 // (equal values), the k-th largest of those collected is a higher bound, and the collection is done again: every key is
 // different, so this ends.
-template <typename T, int BLOCK, int KEPT>
-__device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &sp, float own, int k, float m, float inv_t, float lns, int64_t *index, float *lp,
-                                        TopLds<BLOCK> &t, const uint4 (&kept)[KEPT > 0 ? KEPT : 1], const Slots<BLOCK> *slots, int shift)
+template <typename T, int BLOCK, int KEPT, typename PUT>
+__device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &sp, float own, int k, TopLds<BLOCK> &t, const uint4 (&kept)[KEPT > 0 ? KEPT : 1],
+                                        const Slots<BLOCK> *slots, int shift, PUT put)
 {
     constexpr int V = CHUNK<T>, EACH = BLOCK == 64 ? KEPT : 4;  // groups that a lane compares
     const int tid = threadIdx.x, lane = tid & 63, rest = KEPT > 0 ? sp.hi : sp.lo;
     uint32_t u[EACH], bound = 0;
-    if constexpr (BLOCK == 64) {  // every chunk is a group
+    int groups = EACH;
+    if (BLOCK == 64 && k <= 16) {  // (then 64 groups, the lanes, bound as well)
+        groups = 1;
+        u[0] = ordered(own);
+    } else if constexpr (BLOCK == 64) {  // every chunk is a group
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             float x[V], g = i == 0 && tid < sp.edges ? element(row + sp.edge(tid, n)) : -INFINITY;
@@ -284,7 +288,8 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
         const uint32_t more = bound | (1u << bit);
         int reach = 0;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) reach += __popcll(__ballot(u[i] >= more));
+        for (int i = 0; i < EACH; ++i)
+            if (i < groups) reach += __popcll(__ballot(u[i] >= more));
         if (reach >= k) bound = more;
         if (reach == k) break;
     }
@@ -314,13 +319,17 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
         auto offer_chunk = [&](const uint4 &b, int c) {
             float x[V];
             unpack<T>(b, x);
+            float most = x[0];
+#pragma unroll
+            for (int j = 1; j < V; ++j) most = fmaxf(most, x[j]);
+            if (ordered(most) < (uint32_t)(bar >> 32)) return;
 #pragma unroll
             for (int j = 0; j < V; ++j) offer(x[j], sp.first(c) + j);
         };
         if (able) {
 #pragma unroll
             for (int i = 0; i < KEPT; ++i)
-                if (sp.lo + tid + i * BLOCK < sp.hi && (BLOCK != 64 || u[i] >= bound)) offer_chunk(kept[i], sp.lo + tid + i * BLOCK);
+                if (sp.lo + tid + i * BLOCK < sp.hi) offer_chunk(kept[i], sp.lo + tid + i * BLOCK);
             if (tid < sp.edges) offer(element(row + sp.edge(tid, n)), sp.edge(tid, n));
         }
         const int listed = KEPT > 0 ? 0 : t.listed;
@@ -338,6 +347,7 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
         if (found <= TOP_KEYS) break;
         for (int i = tid; i < TOP_KEYS; i += BLOCK) {
             int above = 0;
+#pragma unroll 8
             for (int j = 0; j < TOP_KEYS; ++j) above += t.keys[j] > t.keys[i];
             if (above == k - 1) t.bar = t.keys[i];
         }
@@ -347,29 +357,166 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
     for (int i = tid; i < found; i += BLOCK) {
         const uint64_t key = t.keys[i];
         int above = 0;
+#pragma unroll 8
         for (int j = 0; j < found; ++j) above += t.keys[j] > key;
-        if (above < k) {
-            index[above] = (int64_t)(uint32_t)~(uint32_t)key;
-            lp[above] = (unordered((uint32_t)(key >> 32)) - m) * inv_t - lns;
-        }
+        if (above < k) put(above, key);
     }
-    for (int i = found + tid; i < k; i += BLOCK) {
-        index[i] = -1;
-        lp[i] = -INFINITY;
+    for (int i = found + tid; i < k; i += BLOCK) put(i, 0);
+}
+
+// An alternative's place in the outputs; a key of 0 is none.
+struct TopOut {
+    int64_t *index;
+    float *lp, m, inv_t, lns;
+    __device__ __forceinline__ void operator()(int i, uint64_t key) const
+    {
+        index[i] = key == 0 ? -1 : (int64_t)(uint32_t)~(uint32_t)key;
+        lp[i] = key == 0 ? -INFINITY : (unordered((uint32_t)(key >> 32)) - m) * inv_t - lns;
     }
+};
+
+// ------------------------------------------------------------------------------------------------ few long rows
+// Where there are fewer rows than the chip has room for, a long row is cut into PARTS_MOST parts (fewer, if they would be shorter
+// than PART_LEAST chunks), each a row of its own to one workgroup: one compute unit takes 28 GB/s from memory (a row of 131072
+// bf16: 9 us).  The next launch joins the parts' sums, in their order, and their largest elements.
+constexpr int PART_LEAST = 1024, PARTS_MOST = 64, SPLIT_ROWS = 512, SPLIT_CHUNKS = 4096;
+struct Parts { int count; int64_t length; };  // elements of a part, a multiple of 64; count = 1: the rows are not split
+
+static Parts row_parts(int dtype, int64_t rows, int64_t classes)
+{
+    const int64_t v = 16 / (int64_t)elem_size(dtype), chunks = classes / v;
+    if (rows >= SPLIT_ROWS || chunks <= SPLIT_CHUNKS) return {1, classes};
+    int64_t length = round_up((classes + PARTS_MOST - 1) / PARTS_MOST, 64);
+    if (length < PART_LEAST * v) length = PART_LEAST * v;
+    return {(int)((classes + length - 1) / length), length};
+}
+
+// bytes of the parts' sums, and of their keys behind them
+static size_t parts_bytes(int dtype, int64_t rows, int64_t classes, int top)
+{
+    const Parts p = row_parts(dtype, 1, classes);
+    const int64_t most = rows < SPLIT_ROWS ? rows : SPLIT_ROWS - 1;  // more rows are not split: a workspace for them serves fewer that are
+    return p.count > 1 ? (size_t)most * p.count * (sizeof(float4) + (size_t)top * sizeof(uint64_t)) : 0;
+}
+size_t logprob_workspace(int dtype, int64_t rows, int64_t classes, int top) { return parts_bytes(dtype, rows, classes, top); }
+size_t distill_workspace(int dtype, int64_t rows, int64_t classes) { return parts_bytes(dtype, rows, classes, 0); }
+
+template <typename T, int KEPT, int ALSO, bool TOP>
+__global__ __launch_bounds__(256) void row_parts_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int n, int parts, int64_t length, float c, int shift, int top,
+                                                        float4 *__restrict__ sums, uint64_t *__restrict__ keys)
+{
+    constexpr int BLOCK = 256;
+    __shared__ float lds[2 * (BLOCK / 64)];
+    __shared__ TopLds<BLOCK> tl;
+    __shared__ Slots<TOP && KEPT == 0 ? BLOCK : 1> sl;
+    Slots<BLOCK> *slots = TOP && KEPT == 0 ? reinterpret_cast<Slots<BLOCK> *>(&sl) : nullptr;
+    const int64_t id = grid_row(), r = id / parts, p = id % parts, begin = p * length;
+    if (r >= rows) return;
+    const T *row = logits + r * ld + begin;
+    const int mine = (int)(begin + length < n ? length : n - begin);
+    const RowSplit<T> sp(row, mine);
+    float own;
+    uint4 kept[KEPT > 0 ? KEPT : 1];
+    const Sums a = row_sums<T, BLOCK, ALSO, true, KEPT>(row, mine, sp, c, &own, lds, kept, slots, shift);
+    if (threadIdx.x == 0) sums[id] = make_float4(a.m, a.s, a.t, 0.f);
+    if (TOP)
+        row_top<T, BLOCK, KEPT>(row, mine, sp, own, top, tl, kept, slots, shift,
+                              [&](int i, uint64_t key) { keys[id * top + i] = key == 0 ? 0 : key - (uint64_t)begin; });  // (the index is stored inverted)
+}
+
+// The sums of a row from its parts', the same in every wavefront.
+template <int ALSO> __device__ __forceinline__ Sums join_parts(const float4 *sums, int parts, float c)
+{
+    const int lane = threadIdx.x & 63;
+    const float4 p = lane < parts ? sums[lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    Sums a = {p.x, 0.f, p.y, p.z};
+    const float m = wave_join(a.m, Max());
+    // (relative to the maxima themselves)
+    if (a.m != m && a.m > -INFINITY) {
+        const float d = a.m - m, z = d * c, f = exp2_fast(z);
+        if (ALSO == Z_TIMES) a.t = f > 0.f ? (a.t + z * a.s) * f : 0.f;
+        if (ALSO >= AT_ONE) a.t *= at_one<ALSO>(f, d);
+        a.s *= f;
+    }
+    a.m = m;
+    a.s = wave_join(a.s, Add());
+    a.t = wave_join(a.t, Add());
+    return a;
+}
+
+// The k largest of the parts' k largest by a workgroup of 256, as in row_top: the k-th largest of the threads' maxima is the bound,
+// here of whole keys, so that few more than k reach it whatever is equal.  found [parts * k].
+template <typename PUT> __device__ __forceinline__ void join_tops(const uint64_t *keys, int total, int k, uint64_t *found, PUT put)
+{
+    __shared__ uint64_t group[256];
+    __shared__ int count;
+    const int tid = threadIdx.x, lane = tid & 63;
+    uint64_t own = 0;
+    for (int i = tid; i < total; i += 256) own = keys[i] > own ? keys[i] : own;
+    group[tid] = own;
+    if (tid == 0) count = 0;
+    __syncthreads();
+    uint64_t g[4], bound = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) g[i] = group[i * 64 + lane];
+    for (int bit = 63; bit >= 0; --bit) {
+        const uint64_t more = bound | (1ull << bit);
+        int reach = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reach += __popcll(__ballot(g[i] >= more));
+        if (reach >= k) bound = more;
+        if (reach == k) break;
+    }
+    if (bound == 0) bound = 1;  // (a key of 0 is none)
+    if (own >= bound)
+        for (int i = tid; i < total; i += 256)
+            if (keys[i] >= bound) found[atomicAdd(&count, 1)] = keys[i];
+    __syncthreads();
+    const int n = count;
+    for (int i = tid; i < n; i += 256) {
+        int above = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) above += found[j] > found[i];
+        if (above < k) put(above, found[i]);
+    }
+    for (int i = n + tid; i < k; i += 256) put(i, 0);
 }
 
 // ------------------------------------------------------------------------------------------------ log probabilities
+struct LogprobOut {
+    const int64_t *targets;
+    int given;
+    float *logprob, *entropy;
+    int top;
+    int64_t *top_index;
+    float *top_logprob, *stats;
+};
+
+// What is written of a row apart from its alternatives; returns ln s.
+template <typename T, int BLOCK, bool ENTROPY> __device__ __forceinline__ float write_logprobs(const LogprobOut &o, const T *row, int64_t r, int n, const Sums &a, float inv_t)
+{
+    const bool none = a.m == -INFINITY && a.s == 0.f;
+    const float lns = logf(a.s);
+    if (threadIdx.x == 0) {
+        if (ENTROPY) o.entropy[r] = none ? 0.f : lns - LN2 * a.t / a.s;
+        if (o.stats != nullptr) o.stats[2 * r] = a.m, o.stats[2 * r + 1] = a.s;
+    }
+    for (int i = threadIdx.x; i < o.given; i += BLOCK) {
+        const int64_t at = o.targets[r * o.given + i];
+        float v = at < 0 ? 0.f : NAN;
+        if (at >= 0 && at < n) v = none ? -INFINITY : (element(row + at) - a.m) * inv_t - lns;
+        o.logprob[r * o.given + i] = v;
+    }
+    return lns;
+}
+
 template <typename T, int BLOCK, int KEPT, bool ENTROPY>
-__global__ __launch_bounds__(BLOCK) void logprob_forward_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int n, float c, float inv_t, int shift,
-                                                                const int64_t *__restrict__ targets, int given, float *__restrict__ logprob, float *__restrict__ entropy,
-                                                                int top, int64_t *__restrict__ top_index, float *__restrict__ top_logprob, float *__restrict__ stats)
+__global__ __launch_bounds__(BLOCK) void logprob_forward_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int n, float c, float inv_t, int shift, LogprobOut o)
 {
     __shared__ float lds[2 * (BLOCK / 64)];
     __shared__ TopLds<BLOCK> tl;
-    constexpr bool WHOLE = KEPT > 0 && BLOCK < 1024;  // this variant is launched for rows that it keeps whole
-    __shared__ Slots<WHOLE ? 1 : BLOCK> sl;
-    Slots<BLOCK> *slots = WHOLE || top == 0 ? nullptr : reinterpret_cast<Slots<BLOCK> *>(&sl);
+    __shared__ Slots<(KEPT > 0) ? 1 : BLOCK> sl;  // rows that are kept whole need none
+    Slots<BLOCK> *slots = KEPT > 0 || o.top == 0 ? nullptr : reinterpret_cast<Slots<BLOCK> *>(&sl);
     const int64_t r = grid_row();
     if (r >= rows) return;
     const T *row = logits + r * ld;
@@ -377,25 +524,19 @@ __global__ __launch_bounds__(BLOCK) void logprob_forward_kernel(const T *__restr
     float own;
     uint4 kept[KEPT > 0 ? KEPT : 1];
     const Sums a = row_sums<T, BLOCK, ENTROPY ? Z_TIMES : NOTHING, true, KEPT>(row, n, sp, c, &own, lds, kept, slots, shift);
-    const float lns = logf(a.s);
-    if (threadIdx.x == 0) {
-        if (ENTROPY) entropy[r] = a.m == -INFINITY && a.s == 0.f ? 0.f : lns - LN2 * a.t / a.s;
-        if (stats != nullptr) stats[2 * r] = a.m, stats[2 * r + 1] = a.s;
-    }
-    for (int i = threadIdx.x; i < given; i += BLOCK) {
-        const int64_t at = targets[r * given + i];
-        float v = at < 0 ? 0.f : NAN;
-        if (at >= 0 && at < n) v = a.m == -INFINITY && a.s == 0.f ? -INFINITY : (element(row + at) - a.m) * inv_t - lns;
-        logprob[r * given + i] = v;
-    }
-    if (top > 0) {
-        if constexpr (WHOLE) {
-            row_top<T, BLOCK, KEPT>(row, n, sp, own, top, a.m, inv_t, lns, top_index + r * top, top_logprob + r * top, tl, kept, slots, shift);
-        } else {
-            uint4 none[1];
-            row_top<T, BLOCK, 0>(row, n, sp, own, top, a.m, inv_t, lns, top_index + r * top, top_logprob + r * top, tl, none, slots, shift);
-        }
-    }
+    const float lns = write_logprobs<T, BLOCK, ENTROPY>(o, row, r, n, a, inv_t);
+    if (o.top > 0) row_top<T, BLOCK, KEPT>(row, n, sp, own, o.top, tl, kept, slots, shift, TopOut{o.top_index + r * o.top, o.top_logprob + r * o.top, a.m, inv_t, lns});
+}
+
+template <typename T, bool ENTROPY>
+__global__ __launch_bounds__(256) void logprob_join_kernel(const T *__restrict__ logits, int64_t ld, int n, int parts, float c, float inv_t, const float4 *__restrict__ sums,
+                                                           const uint64_t *__restrict__ keys, LogprobOut o)
+{
+    extern __shared__ uint64_t tops[];
+    const int64_t r = blockIdx.x;
+    const Sums a = join_parts<ENTROPY ? Z_TIMES : NOTHING>(sums + r * parts, parts, c);
+    const float lns = write_logprobs<T, 256, ENTROPY>(o, logits + r * ld, r, n, a, inv_t);
+    if (o.top > 0) join_tops(keys + r * parts * o.top, parts * o.top, o.top, tops, TopOut{o.top_index + r * o.top, o.top_logprob + r * o.top, a.m, inv_t, lns});
 }
 
 // ------------------------------------------------------------------------------------------------ gradients
@@ -526,49 +667,60 @@ int launch_logprob_backward(const LogitsArgs &a, const int64_t *targets, int giv
                                 : logprob_backward<float>(a, targets, given, dlogprob, dentropy, entropy, stats, (float *)out, ld_out, s);
 }
 
-// Threads per row: one wavefront for short rows, so that many rows share a compute unit without barriers; 1024 where the
-// rows are too few to occupy the chip otherwise.
-static int row_block(const LogitsArgs &a)
+// Slots of 2^shift batches, at most SLOTS of them for a row that may begin anywhere in its first chunk.
+static int slot_shift(int64_t chunks, int block)
 {
-    const int64_t chunks = a.classes * (int64_t)elem_size(a.dtype) / 16;
-    if (chunks <= 256) return 64;
-    return a.rows < 512 && chunks > 1024 ? 1024 : 256;
+    int shift = 0;
+    while (((chunks / (BATCH * block)) >> shift) + 1 > SLOTS) ++shift;
+    return shift;
 }
 
-#define OMNI_BY_TYPE_AND_BLOCK(LAUNCH)              \
-    do {                                            \
-        const int block = row_block(a);             \
-        if (a.dtype == OMNI_BF16) {                 \
-            if (block == 64) LAUNCH(bf16_t, 64);    \
-            else if (block == 256) LAUNCH(bf16_t, 256); \
-            else LAUNCH(bf16_t, 1024);              \
-        } else {                                    \
-            if (block == 64) LAUNCH(float, 64);     \
-            else if (block == 256) LAUNCH(float, 256); \
-            else LAUNCH(float, 1024);               \
-        }                                           \
+// The parts' launch: their sums, and with top > 0 their largest elements.
+template <typename T, int ALSO> static int launch_parts(const LogitsArgs &a, const Parts &p, float c, int top, float4 *sums, uint64_t *keys, hipStream_t s)
+{
+    const int64_t chunks = p.length / CHUNK<T>;
+    const int shift = slot_shift(chunks, 256);
+    const dim3 grid = row_grid(a.rows * p.count);
+#define OMNI_PARTS(K, TOP) \
+    hipLaunchKernelGGL((row_parts_kernel<T, K, ALSO, TOP>), grid, dim3(256), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, p.count, p.length, c, shift, top, sums, keys)
+#define OMNI_PARTS_BY_LENGTH(TOP)                 \
+    do {                                          \
+        if (chunks <= 4 * 256) OMNI_PARTS(4, TOP); \
+        else OMNI_PARTS(0, TOP);                  \
     } while (0)
+    if constexpr (ALSO == NOTHING || ALSO == Z_TIMES) {
+        if (top > 0) OMNI_PARTS_BY_LENGTH(true);
+        else OMNI_PARTS_BY_LENGTH(false);
+    } else {
+        OMNI_PARTS_BY_LENGTH(false);
+    }
+#undef OMNI_PARTS_BY_LENGTH
+#undef OMNI_PARTS
+    OMNI_LAUNCH_CHECK();
+    return OMNI_OK;
+}
 
-template <typename T> static int logprob_forward(const LogitsArgs &a, const int64_t *targets, int given, float *logprob, float *entropy, int top, int64_t *top_index,
-                                                float *top_logprob, float *stats, hipStream_t s)
+template <typename T, bool ENTROPY> static int logprob_forward(const LogitsArgs &a, const LogprobOut &o, void *workspace, hipStream_t s)
 {
     const int64_t chunks = a.classes / CHUNK<T>;
     const float inv_t = 1.f / a.temperature, c = LOG2E / a.temperature;
-#define OMNI_LOGPROB(B, K)                                                                                                                                                    \
-    do {                                                                                                                                                                      \
-        int shift = 0; /* at most SLOTS slots; one chunk more than the row has, since chunks begin at an aligned address */                                                    \
-        while (((chunks / (BATCH * B)) >> shift) + 1 > SLOTS) ++shift;                                                                                                         \
-        if (entropy != nullptr)                                                                                                                                               \
-            hipLaunchKernelGGL((logprob_forward_kernel<T, B, K, true>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, c, inv_t, shift, targets, \
-                               given, logprob, entropy, top, top_index, top_logprob, stats);                                                                                  \
-        else                                                                                                                                                                  \
-            hipLaunchKernelGGL((logprob_forward_kernel<T, B, K, false>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, c, inv_t, shift, targets, \
-                               given, logprob, entropy, top, top_index, top_logprob, stats);                                                                                  \
-    } while (0)
+    const Parts p = row_parts(a.dtype, a.rows, a.classes);
+    if (p.count > 1) {
+        float4 *sums = (float4 *)workspace;
+        uint64_t *keys = (uint64_t *)(sums + a.rows * p.count);
+        const int st = launch_parts<T, ENTROPY ? Z_TIMES : NOTHING>(a, p, c, o.top, sums, keys, s);
+        if (st != OMNI_OK) return st;
+        hipLaunchKernelGGL((logprob_join_kernel<T, ENTROPY>), dim3((unsigned)a.rows), dim3(256), (size_t)p.count * o.top * sizeof(uint64_t), s, (const T *)a.logits, a.ld, (int)a.classes,
+                           p.count, c, inv_t, sums, keys, o);
+        OMNI_LAUNCH_CHECK();
+        return OMNI_OK;
+    }
+    // short rows stay with one wavefront, which needs no barriers
+#define OMNI_LOGPROB(B, K) \
+    hipLaunchKernelGGL((logprob_forward_kernel<T, B, K, ENTROPY>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, c, inv_t, slot_shift(chunks, B), o)
     if (chunks <= 256) OMNI_LOGPROB(64, 4);
     else if (chunks <= 512) OMNI_LOGPROB(64, 8);
     else if (chunks <= 1024) OMNI_LOGPROB(256, 4);
-    else if (a.rows < 512) OMNI_LOGPROB(1024, 16);
     else OMNI_LOGPROB(256, 0);
 #undef OMNI_LOGPROB
     OMNI_LAUNCH_CHECK();
@@ -576,11 +728,12 @@ template <typename T> static int logprob_forward(const LogitsArgs &a, const int6
 }
 
 int launch_logprob_forward(const LogitsArgs &a, const int64_t *targets, int given, float *logprob, float *entropy, int top, int64_t *top_index, float *top_logprob,
-                           float *stats, hipStream_t s)
+                           float *stats, void *workspace, hipStream_t s)
 {
     ProfScope prof(KID_LOGPROB, s, 0.0, (double)a.rows * a.classes * elem_size(a.dtype));
-    return a.dtype == OMNI_BF16 ? logprob_forward<bf16_t>(a, targets, given, logprob, entropy, top, top_index, top_logprob, stats, s)
-                                : logprob_forward<float>(a, targets, given, logprob, entropy, top, top_index, top_logprob, stats, s);
+    const LogprobOut o = {targets, given, logprob, entropy, top, top_index, top_logprob, stats};
+    if (a.dtype == OMNI_BF16) return entropy != nullptr ? logprob_forward<bf16_t, true>(a, o, workspace, s) : logprob_forward<bf16_t, false>(a, o, workspace, s);
+    return entropy != nullptr ? logprob_forward<float, true>(a, o, workspace, s) : logprob_forward<float, false>(a, o, workspace, s);
 }
 
 // ------------------------------------------------------------------------------------------------ distillation
@@ -688,6 +841,20 @@ template <int ALSO> struct Gradient {
     }
 };
 
+// The loss of a row and what the backward pass needs of it, from the row's sums; returns the row's entries.
+template <typename T, int BLOCK, int ALSO>
+__device__ __forceinline__ Entries write_loss(const DistillArgs &d, const T *row, int64_t r, int n, const Sums &a, float *loss, float *stats, EntryLds &l, float *lds)
+{
+    const Entries e = read_entries<BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
+    __syncthreads();
+    const float v = row_loss<T, BLOCK, ALSO != NOTHING>(d, row, r, n, a, e, l, lds);
+    if (threadIdx.x == 0) {
+        loss[r] = v;
+        if (stats != nullptr) stats[4 * r] = a.m, stats[4 * r + 1] = a.s, stats[4 * r + 2] = ALSO != NOTHING ? a.t : a.s, stats[4 * r + 3] = 0.f;
+    }
+    return e;
+}
+
 // Whole rows: the loss alone.
 template <typename T, int BLOCK, int ALSO>
 __global__ __launch_bounds__(BLOCK) void distill_loss_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int n, DistillArgs d, float c, float *__restrict__ loss,
@@ -701,13 +868,19 @@ __global__ __launch_bounds__(BLOCK) void distill_loss_kernel(const T *__restrict
     const RowSplit<T> sp(row, n);
     uint4 none[1];
     const Sums a = row_sums<T, BLOCK, ALSO, true, 0>(row, n, sp, c, nullptr, lds, none);
-    const Entries e = read_entries<BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
-    __syncthreads();
-    const float v = row_loss<T, BLOCK, ALSO != NOTHING>(d, row, r, n, a, e, l, lds);
-    if (threadIdx.x == 0) {
-        loss[r] = v;
-        if (stats != nullptr) stats[4 * r] = a.m, stats[4 * r + 1] = a.s, stats[4 * r + 2] = ALSO != NOTHING ? a.t : a.s, stats[4 * r + 3] = 0.f;
-    }
+    write_loss<T, BLOCK, ALSO>(d, row, r, n, a, loss, stats, l, lds);
+}
+
+// ... of rows whose sums the parts' launch has taken
+template <typename T, int ALSO>
+__global__ __launch_bounds__(GRAD_BLOCK) void distill_join_kernel(const T *__restrict__ logits, int64_t ld, int n, int parts, DistillArgs d, float c, const float4 *__restrict__ sums,
+                                                          float *__restrict__ loss, float *__restrict__ stats)
+{
+    __shared__ float lds[2 * (GRAD_BLOCK / 64)];
+    __shared__ EntryLds l;
+    const int64_t r = blockIdx.x;
+    const Sums a = join_parts<ALSO>(sums + r * parts, parts, c);
+    write_loss<T, GRAD_BLOCK, ALSO>(d, logits + r * ld, r, n, a, loss, stats, l, lds);
 }
 
 // Loss and gradient of whole rows.  The row's first KEPT chunks a thread stay in registers from the sums to the gradient; what
@@ -726,10 +899,7 @@ __global__ __launch_bounds__(BLOCK) void distill_both_kernel(const T *logits, in
     const RowSplit<T> sp(row, n);
     uint4 kept[KEPT];
     const Sums a = row_sums<T, BLOCK, ALSO, false, KEPT>(row, n, sp, c, nullptr, lds, kept);
-    const Entries e = read_entries<BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
-    __syncthreads();
-    const float v = row_loss<T, BLOCK, ALSO != NOTHING>(d, row, r, n, a, e, l, lds);
-    if (threadIdx.x == 0) loss[r] = v;
+    const Entries e = write_loss<T, BLOCK, ALSO>(d, row, r, n, a, loss, nullptr, l, lds);
     const Coefs k = row_coefs<BLOCK, ALSO != NOTHING>(d, r, n, a.m, a.s, a.t, e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
     const Gradient<ALSO> value(k, a.m, c);
     ListedOut<T, BLOCK, KEPT_MOST + 1> listed;
@@ -755,9 +925,12 @@ __global__ __launch_bounds__(BLOCK) void distill_both_kernel(const T *logits, in
     listed.write(to, l, k.count, value);
 }
 
+// The gradient from given sums: the statistics of an earlier call, or (sums != null) the parts' of this one.  loss != null: the
+// row's first workgroup writes the loss, too, for which it reads all over the row -- not where the row is overwritten.
 template <typename T, int ALSO>
 __global__ __launch_bounds__(GRAD_BLOCK) void distill_backward_kernel(const T *logits, int64_t ld, int64_t rows, int n, int pieces, DistillArgs d, float c,
-                                                                      const float *__restrict__ stats, T *out, int64_t ld_out)
+                                                                      const float *__restrict__ stats, const float4 *__restrict__ sums, int parts, float *__restrict__ loss,
+                                                                      T *out, int64_t ld_out)
 {
     __shared__ float lds[2 * (GRAD_BLOCK / 64)];
     __shared__ EntryLds l;
@@ -766,11 +939,18 @@ __global__ __launch_bounds__(GRAD_BLOCK) void distill_backward_kernel(const T *l
     const int64_t c0 = (id % pieces) * GRAD_CHUNKS, c1 = c0 + GRAD_CHUNKS;
     const T *in = logits + r * ld;
     T *to = out + r * ld_out;
-    const float m = stats[4 * r];
+    Sums a;
+    if (sums != nullptr) a = join_parts<ALSO>(sums + r * parts, parts, c);
+    else a = {stats[4 * r], 0.f, stats[4 * r + 1], stats[4 * r + 2]};
     const Entries e = read_entries<GRAD_BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
     __syncthreads();
-    const Coefs k = row_coefs<GRAD_BLOCK, ALSO != NOTHING>(d, r, n, m, stats[4 * r + 1], stats[4 * r + 2], e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
-    const Gradient<ALSO> value(k, m, c);
+    if (loss != nullptr && c0 == 0) {
+        const float v = row_loss<T, GRAD_BLOCK, ALSO != NOTHING>(d, in, r, n, a, e, l, lds);
+        if (threadIdx.x == 0) loss[r] = v;
+        __syncthreads();
+    }
+    const Coefs k = row_coefs<GRAD_BLOCK, ALSO != NOTHING>(d, r, n, a.m, a.s, a.t, e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
+    const Gradient<ALSO> value(k, a.m, c);
     ListedOut<T, GRAD_BLOCK, KEPT_MOST + 1> listed;
     listed.read(in, to, n, c0, c1, l, k.count);
     __syncthreads();
@@ -798,28 +978,79 @@ static Also second_softmax(const DistillArgs &d)
 
 static float distill_scale(const DistillArgs &d) { return LOG2E / (d.alpha > 0.f && d.kept > 0 ? d.temperature : 1.f); }
 
-int launch_distill_loss(const LogitsArgs &a, const DistillArgs &d, float *loss, float *stats, hipStream_t s)
+template <typename T> static int distill_loss(const LogitsArgs &a, const DistillArgs &d, float *loss, float *stats, void *workspace, hipStream_t s)
 {
-    ProfScope prof(KID_DISTILL, s, 0.0, (double)a.rows * a.classes * elem_size(a.dtype));
     const float c = distill_scale(d);
-#define OMNI_DISTILL_LOSS(T, B, ALSO) \
+    const int64_t chunks = a.classes / CHUNK<T>;
+    const Parts p = row_parts(a.dtype, a.rows, a.classes);
+    if (p.count > 1) {
+        float4 *sums = (float4 *)workspace;
+        int st = OMNI_OK;
+#define OMNI_DISTILL_PARTS(UNUSED, ALSO)                                                                                                                                 \
+    do {                                                                                                                                                                 \
+        if ((st = launch_parts<T, ALSO>(a, p, c, 0, sums, nullptr, s)) != OMNI_OK) return st;                                                                            \
+        hipLaunchKernelGGL((distill_join_kernel<T, ALSO>), dim3((unsigned)a.rows), dim3(GRAD_BLOCK), 0, s, (const T *)a.logits, a.ld, (int)a.classes, p.count, d, c, sums, loss, stats); \
+    } while (0)
+        OMNI_BY_SECOND(OMNI_DISTILL_PARTS, 0);
+#undef OMNI_DISTILL_PARTS
+        OMNI_LAUNCH_CHECK();
+        return OMNI_OK;
+    }
+#define OMNI_DISTILL_LOSS(B, ALSO) \
     hipLaunchKernelGGL((distill_loss_kernel<T, B, ALSO>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, d, c, loss, stats)
-#define OMNI_DISTILL_LOSS2(T, B) OMNI_BY_SECOND(OMNI_DISTILL_LOSS, T, B)
-    OMNI_BY_TYPE_AND_BLOCK(OMNI_DISTILL_LOSS2);
-#undef OMNI_DISTILL_LOSS2
+    if (chunks <= 512) OMNI_BY_SECOND(OMNI_DISTILL_LOSS, 64);
+    else OMNI_BY_SECOND(OMNI_DISTILL_LOSS, 256);
 #undef OMNI_DISTILL_LOSS
     OMNI_LAUNCH_CHECK();
     return OMNI_OK;
 }
 
-template <typename T> static int distill_both(const LogitsArgs &a, const DistillArgs &d, float *loss, T *out, int64_t ld_out, hipStream_t s)
+int launch_distill_loss(const LogitsArgs &a, const DistillArgs &d, float *loss, float *stats, void *workspace, hipStream_t s)
+{
+    ProfScope prof(KID_DISTILL, s, 0.0, (double)a.rows * a.classes * elem_size(a.dtype));
+    return a.dtype == OMNI_BF16 ? distill_loss<bf16_t>(a, d, loss, stats, workspace, s) : distill_loss<float>(a, d, loss, stats, workspace, s);
+}
+
+template <typename T>
+static int distill_backward(const LogitsArgs &a, const DistillArgs &d, const float *stats, const float4 *sums, int parts, float *loss, T *out, int64_t ld_out, hipStream_t s)
+{
+    const float c = distill_scale(d);
+    const int pieces = (int)(((a.classes + CHUNK<T> - 1) / CHUNK<T> + 1 + GRAD_CHUNKS - 1) / GRAD_CHUNKS);
+#define OMNI_DISTILL_BACKWARD(B, ALSO)                                                                                                                              \
+    hipLaunchKernelGGL((distill_backward_kernel<T, ALSO>), row_grid(a.rows * pieces), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, d, c, stats, \
+                       sums, parts, loss, out, ld_out)
+    OMNI_BY_SECOND(OMNI_DISTILL_BACKWARD, GRAD_BLOCK);
+#undef OMNI_DISTILL_BACKWARD
+    OMNI_LAUNCH_CHECK();
+    return OMNI_OK;
+}
+
+template <typename T> static int distill_both(const LogitsArgs &a, const DistillArgs &d, float *loss, T *out, int64_t ld_out, void *workspace, hipStream_t s)
 {
     const float c = distill_scale(d);
     const int64_t chunks = a.classes / CHUNK<T>;
+    const Parts p = row_parts(a.dtype, a.rows, a.classes);
+    if (p.count > 1) {
+        float4 *sums = (float4 *)workspace;
+        int st = OMNI_OK;
+        const bool over = (const void *)out == a.logits;
+#define OMNI_DISTILL_PARTS(UNUSED, ALSO)                                                                                                                                 \
+    do {                                                                                                                                                                 \
+        if ((st = launch_parts<T, ALSO>(a, p, c, 0, sums, nullptr, s)) != OMNI_OK) return st;                                                                            \
+        if (over)                                                                                                                                                        \
+            hipLaunchKernelGGL((distill_join_kernel<T, ALSO>), dim3((unsigned)a.rows), dim3(GRAD_BLOCK), 0, s, (const T *)a.logits, a.ld, (int)a.classes, p.count, d, c, sums,   \
+                               loss, nullptr);                                                                                                                           \
+    } while (0)
+        OMNI_BY_SECOND(OMNI_DISTILL_PARTS, 0);
+#undef OMNI_DISTILL_PARTS
+        OMNI_LAUNCH_CHECK();
+        return distill_backward<T>(a, d, nullptr, sums, p.count, over ? nullptr : loss, out, ld_out, s);
+    }
 #define OMNI_DISTILL_BOTH(B, K, ALSO) \
     hipLaunchKernelGGL((distill_both_kernel<T, B, K, ALSO>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, d, c, loss, out, ld_out)
     if (chunks <= 256) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 64, 4);
     else if (chunks <= 1024) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 256, 4);
+    else if (chunks <= 2048) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 256, 8);
     else if (chunks <= 4096) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 256, 16);
     else if (chunks <= 8192) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 512, 16);
     else OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 1024, 16);
@@ -828,29 +1059,17 @@ template <typename T> static int distill_both(const LogitsArgs &a, const Distill
     return OMNI_OK;
 }
 
-int launch_distill_both(const LogitsArgs &a, const DistillArgs &d, float *loss, void *out, int64_t ld_out, hipStream_t s)
+int launch_distill_both(const LogitsArgs &a, const DistillArgs &d, float *loss, void *out, int64_t ld_out, void *workspace, hipStream_t s)
 {
     ProfScope prof(KID_DISTILL, s, 0.0, 2.0 * (double)a.rows * a.classes * elem_size(a.dtype));
-    return a.dtype == OMNI_BF16 ? distill_both<bf16_t>(a, d, loss, (bf16_t *)out, ld_out, s) : distill_both<float>(a, d, loss, (float *)out, ld_out, s);
-}
-
-template <typename T> static int distill_backward(const LogitsArgs &a, const DistillArgs &d, const float *stats, T *out, int64_t ld_out, hipStream_t s)
-{
-    const float c = distill_scale(d);
-    const int pieces = (int)(((a.classes + CHUNK<T> - 1) / CHUNK<T> + 1 + GRAD_CHUNKS - 1) / GRAD_CHUNKS);
-#define OMNI_DISTILL_BACKWARD(B, ALSO)                                                                                                                              \
-    hipLaunchKernelGGL((distill_backward_kernel<T, ALSO>), row_grid(a.rows * pieces), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, d, c, stats, \
-                       out, ld_out)
-    OMNI_BY_SECOND(OMNI_DISTILL_BACKWARD, GRAD_BLOCK);
-#undef OMNI_DISTILL_BACKWARD
-    OMNI_LAUNCH_CHECK();
-    return OMNI_OK;
+    return a.dtype == OMNI_BF16 ? distill_both<bf16_t>(a, d, loss, (bf16_t *)out, ld_out, workspace, s) : distill_both<float>(a, d, loss, (float *)out, ld_out, workspace, s);
 }
 
 int launch_distill_backward(const LogitsArgs &a, const DistillArgs &d, const float *stats, void *out, int64_t ld_out, hipStream_t s)
 {
     ProfScope prof(KID_DISTILL, s, 0.0, 2.0 * (double)a.rows * a.classes * elem_size(a.dtype));
-    return a.dtype == OMNI_BF16 ? distill_backward<bf16_t>(a, d, stats, (bf16_t *)out, ld_out, s) : distill_backward<float>(a, d, stats, (float *)out, ld_out, s);
+    return a.dtype == OMNI_BF16 ? distill_backward<bf16_t>(a, d, stats, nullptr, 0, nullptr, (bf16_t *)out, ld_out, s)
+                                : distill_backward<float>(a, d, stats, nullptr, 0, nullptr, (float *)out, ld_out, s);
 }
 
 }  // namespace omni

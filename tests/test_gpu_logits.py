@@ -123,6 +123,29 @@ def test_logprob_lengths(B, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n", [(1, 32769), (5, 65541), (2, 700001), (511, 33000), (512, 33000)])
+def test_few_long_rows_in_parts(B, rows, n, dtype):
+    # parts that end inside a chunk, more parts than a row may have, and both sides of the number of rows that are split; rows
+    # whose largest elements lie in one part, in ties across all parts, and parts without any possible class
+    x = logits(rows, n, dtype, seed=rows)
+    x[0, 5000:15000] = 20.0
+    x[-1, ::977] = 25.0
+    if rows > 3:
+        x[1, 9000:] = -float("inf")
+        x[2] = -float("inf")
+        x[2, n - 1] = 1.0
+        x[3, n // 2] = float("nan")
+    g = torch.Generator().manual_seed(5)
+    targets = torch.randint(0, n, (rows, 2), generator=g).cuda()
+    check_logprob(B, x, targets, 40, 0.8, 3, torch.randn(rows, 2, generator=g).cuda())
+    check_logprob(B, x, targets, 0, 1.0)
+    if rows > 3:
+        x[3, n // 2] = 0.0
+    for temperature, alpha in ((2.0, 0.5), (3.0, 0.5), (1.0, 1.0)):
+        check_distill(B, x, *teacher(rows, n, 7, 2), temperature, alpha, 1 if temperature == 1.0 else 0)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("rows,n,top", [(700, 40, 3), (520, 9001, 20), (1030, 2600, 0), (257, 1000, 5)])
 def test_logprob_many_rows(B, rows, n, top, dtype):
     x = logits(rows, n, dtype, masked=0.1)

@@ -28,30 +28,34 @@ def norm_backward(L, dtype=0, rows=4, width=8, x=P, ldx=8, dy=P, lddy=8, gamma=P
     return L.omni_layer_norm_backward(dtype, rows, width, x, ldx, dy, lddy, gamma, mean, rstd, dx, lddx, dgamma, dbeta, ws, nws, None)
 
 
-def logprob_forward(L, dtype=0, rows=4, classes=8, x=P, ld=8, t=1.0, targets=P, given=1, lp=P, entropy=P, top=2, index=P, best=P, stats=P):
-    return L.omni_logprob_forward(dtype, rows, classes, x, ld, F(t), targets, given, lp, entropy, top, index, best, stats, None)
+def logprob_forward(L, dtype=0, rows=4, classes=8, x=P, ld=8, t=1.0, targets=P, given=1, lp=P, entropy=P, top=2, index=P, best=P, stats=P, ws=P, nws=BIG):
+    return L.omni_logprob_forward(dtype, rows, classes, x, ld, F(t), targets, given, lp, entropy, top, index, best, stats, ws, nws, None)
 
 
 def logprob_backward(L, dtype=0, rows=4, classes=8, x=P, ld=8, t=1.0, stats=P, targets=P, given=1, dlp=P, dh=P, h=P, out=P, ldo=8):
     return L.omni_logprob_backward(dtype, rows, classes, x, ld, F(t), stats, targets, given, dlp, dh, h, out, ldo, None)
 
 
-def distill_forward(L, dtype=0, rows=4, classes=8, x=P, ld=8, index=P, values=P, kept=3, labels=P, t=1.0, alpha=0.5, loss=P, stats=P):
-    return L.omni_distill_forward(dtype, rows, classes, x, ld, index, values, kept, labels, F(t), F(alpha), loss, stats, None)
+def distill_forward(L, dtype=0, rows=4, classes=8, x=P, ld=8, index=P, values=P, kept=3, labels=P, t=1.0, alpha=0.5, loss=P, stats=P, ws=P, nws=BIG):
+    return L.omni_distill_forward(dtype, rows, classes, x, ld, index, values, kept, labels, F(t), F(alpha), loss, stats, ws, nws, None)
 
 
 def distill_backward(L, dtype=0, rows=4, classes=8, x=P, ld=8, index=P, values=P, kept=3, labels=P, t=1.0, alpha=0.5, stats=P, dloss=P, scale=1.0, out=P, ldo=8):
     return L.omni_distill_backward(dtype, rows, classes, x, ld, index, values, kept, labels, F(t), F(alpha), stats, dloss, F(scale), out, ldo, None)
 
 
-def distill_both(L, dtype=0, rows=4, classes=8, x=P, ld=8, index=P, values=P, kept=3, labels=P, t=1.0, alpha=0.5, dloss=P, scale=1.0, loss=P, out=P, ldo=8):
-    return L.omni_distill_forward_backward(dtype, rows, classes, x, ld, index, values, kept, labels, F(t), F(alpha), dloss, F(scale), loss, out, ldo, None)
+def distill_both(L, dtype=0, rows=4, classes=8, x=P, ld=8, index=P, values=P, kept=3, labels=P, t=1.0, alpha=0.5, dloss=P, scale=1.0, loss=P, out=P, ldo=8, ws=P,
+                 nws=BIG):
+    return L.omni_distill_forward_backward(dtype, rows, classes, x, ld, index, values, kept, labels, F(t), F(alpha), dloss, F(scale), loss, out, ldo, ws, nws, None)
 
 
 NAN, INF = float("nan"), float("inf")
 SHAPE = [(dict(dtype=2), -2), (dict(rows=-1), -1), (dict(rows=1 << 31), -2)]
 CLASSES = SHAPE + [(dict(classes=0), -1), (dict(classes=(1 << 30) + 1, ld=1 << 31), -2), (dict(rows=1 << 20, classes=1 << 30, ld=1 << 30), -2), (dict(ld=7), -1),
                    (dict(x=None), -1), (dict(x=ODD), -4), (dict(t=0.0), -1), (dict(t=-1.0), -1), (dict(t=NAN), -1), (dict(t=INF), -1), (dict(t=1e-35), -1)]
+
+
+LONG = [(dict(classes=131072, ld=131072, ws=None), -1), (dict(classes=131072, ld=131072, nws=0), -3)]  # rows that are worked on in parts
 
 
 @pytest.mark.parametrize("change,status", SHAPE + [
@@ -72,7 +76,7 @@ def test_layer_norm_backward_refuses(L, change, status):
 
 @pytest.mark.parametrize("change,status", CLASSES + [
     (dict(given=-1), -1), (dict(top=-1), -1), (dict(given=1025), -2), (dict(top=65), -2), (dict(targets=None), -1), (dict(lp=None), -1), (dict(index=None), -1),
-    (dict(best=None), -1)] + [(dict([(k, ODD)]), -4) for k in ("targets", "lp", "entropy", "index", "best", "stats")])
+    (dict(best=None), -1)] + [(dict([(k, ODD)]), -4) for k in ("targets", "lp", "entropy", "index", "best", "stats", "ws")] + LONG)
 def test_logprob_forward_refuses(L, change, status):
     assert logprob_forward(L, **change) == status
 
@@ -89,7 +93,7 @@ PARTS = [(dict(kept=-1), -1), (dict(kept=257), -2), (dict(index=None), -1), (dic
     + [(dict([(k, ODD)]), -4) for k in ("index", "values", "labels")]
 
 
-@pytest.mark.parametrize("change,status", CLASSES + PARTS + [(dict(loss=None), -1), (dict(loss=ODD), -4), (dict(stats=ODD), -4)])
+@pytest.mark.parametrize("change,status", CLASSES + PARTS + [(dict(loss=None), -1), (dict(loss=ODD), -4), (dict(stats=ODD), -4), (dict(ws=ODD), -4)] + LONG)
 def test_distill_forward_refuses(L, change, status):
     assert distill_forward(L, **change) == status
 
@@ -101,7 +105,8 @@ def test_distill_backward_refuses(L, change, status):
 
 
 @pytest.mark.parametrize("change,status", CLASSES + PARTS + [(dict(loss=None), -1), (dict(out=None), -1), (dict(ldo=7), -1), (dict(ldo=9), -1)]
-                         + [(dict([(k, ODD)]), -4) for k in ("loss", "dloss", "out")])
+                         + [(dict([(k, ODD)]), -4) for k in ("loss", "dloss", "out", "ws")]
+                         + [(dict(ldo=131072, **c), st) for c, st in LONG])
 def test_distill_both_refuses(L, change, status):
     assert distill_both(L, **change) == status
 
@@ -110,19 +115,23 @@ def test_no_rows_need_no_buffers(L):
     nothing = dict(rows=0, x=None)
     assert norm_forward(L, y=None, mean=None, rstd=None, **nothing) == 0
     assert norm_backward(L, dy=None, mean=None, rstd=None, dgamma=None, dbeta=None, ws=None, nws=0, **nothing) == 0
-    assert logprob_forward(L, targets=None, lp=None, index=None, best=None, **nothing) == 0
+    assert logprob_forward(L, targets=None, lp=None, index=None, best=None, ws=None, nws=0, **nothing) == 0
     assert logprob_backward(L, stats=None, targets=None, dlp=None, out=None, **nothing) == 0
-    assert distill_forward(L, index=None, values=None, loss=None, **nothing) == 0
+    assert distill_forward(L, index=None, values=None, loss=None, ws=None, nws=0, **nothing) == 0
     assert distill_backward(L, index=None, values=None, stats=None, out=None, **nothing) == 0
-    assert distill_both(L, index=None, values=None, loss=None, out=None, **nothing) == 0
+    assert distill_both(L, index=None, values=None, loss=None, out=None, ws=None, nws=0, **nothing) == 0
 
 
 def test_workspace_never_shrinks_with_more_rows(B, L):
     for dtype in (torch.float32, torch.bfloat16):
         for width in (1, 33, 1000, 4096, 131072):
-            sizes = [B.layer_norm_workspace_bytes(r, width, dtype) for r in (0, 1, 2, 3, 7, 16, 31, 63, 64, 65, 100, 255, 256, 500, 513, 1000, 1024, 5000, 70000)]
-            assert sizes == sorted(sizes), (width, dtype)
+            for size in (lambda r: B.layer_norm_workspace_bytes(r, width, dtype), lambda r: B.logprob_workspace_bytes(r, width, 64, dtype),
+                         lambda r: B.distill_workspace_bytes(r, width, dtype)):
+                sizes = [size(r) for r in (0, 1, 2, 3, 7, 16, 31, 63, 64, 65, 100, 255, 256, 500, 511, 512, 513, 1000, 1024, 5000, 70000)]
+                assert sizes == sorted(sizes), (width, dtype)
     b = ctypes.c_size_t()
+    assert L.omni_logprob_workspace_bytes(0, 4, 8, 65, ctypes.byref(b)) == -2 and L.omni_logprob_workspace_bytes(0, 4, 8, -1, ctypes.byref(b)) == -1
+    assert L.omni_distill_workspace_bytes(0, 4, 0, ctypes.byref(b)) == -1 and L.omni_distill_workspace_bytes(0, 4, 8, None) == -1
     assert L.omni_layer_norm_workspace_bytes(0, 4, 8, None) == -1 and L.omni_layer_norm_workspace_bytes(3, 4, 8, ctypes.byref(b)) == -2
 
 
