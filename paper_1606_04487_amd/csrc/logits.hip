@@ -548,18 +548,29 @@ template <int MOST> struct ListLds {
     float add[MOST];
 };
 
-// Elements [begin, end) of a row, both multiples of the chunk: the chunks are aligned as the output's row is.
-template <typename T, int BLOCK, typename F> __device__ __forceinline__ void write_row(const T *in, T *out, int n, int64_t c0, int64_t c1, F value)
+// Chunks [c0, c1) of a row, aligned as the output's row is, AHEAD of them loaded before the first is used; `also` may change a
+// chunk's values before they are rounded.
+template <typename T, int BLOCK, int AHEAD, typename F, typename G> __device__ __forceinline__ void write_row(const T *in, T *out, int n, int64_t c0, int64_t c1, F value, G also)
 {
     constexpr int V = CHUNK<T>;
     const int shift = (int)(((uintptr_t)out / sizeof(T)) % V);
-    for (int64_t c = c0 + threadIdx.x; c < c1; c += BLOCK) {
-        const int at = (int)(c * V) - shift;
-        float x[V];
-        load_chunk(in, at, n, 0.f, x);
+    if (c1 > (n + shift + V - 1) / V) c1 = (n + shift + V - 1) / V;
+    for (int64_t c = c0 + threadIdx.x; c < c1; c += AHEAD * BLOCK) {
+        Raw<T> b[AHEAD];
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = value(x[j]);
-        store_chunk(out, at, n, x);
+        for (int u = 0; u < AHEAD; ++u) b[u] = load_raw(in, (int)((c + u * BLOCK < c1 ? c + u * BLOCK : c) * V) - shift, n);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (c + u * BLOCK >= c1) break;
+            const int at = (int)((c + u * BLOCK) * V) - shift;
+            float x[V];
+            settle<true>(b[u], at, n);
+            unpack(b[u].w, x);
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[j] = value(x[j]);
+            also(at, x);
+            store_chunk(out, at, n, x);
+        }
     }
 }
 
@@ -608,42 +619,71 @@ template <typename T, int BLOCK, int MOST> struct ListedOut {
     }
 };
 
-constexpr int GRAD_BLOCK = 256, GRAD_CHUNKS = 4 * GRAD_BLOCK;  // chunks of a row that a workgroup writes
+// A workgroup writes 4 chunks a thread of a row (distillation's gradient of 4096 x 65536 bf16: 184 us, 262 with 16 chunks a
+// thread).  One wavefront where that is the row, which then needs no barriers (log probabilities' of 16384 x 1000 bf16: 57 us with
+// workgroups of 256, 14 so).
+struct Pieces { int block, count, chunks; };  // chunks of a piece
 
-template <typename T>
-__global__ __launch_bounds__(GRAD_BLOCK) void logprob_backward_kernel(const T *logits, int64_t ld, int64_t rows, int n, int pieces, float c, float inv_t,
-                                                                      const int64_t *__restrict__ targets, int given, const float *__restrict__ dlogprob,
-                                                                      const float *__restrict__ dentropy, const float *__restrict__ entropy, const float *__restrict__ stats,
-                                                                      T *out, int64_t ld_out)
+static Pieces grad_pieces(int64_t classes, int64_t v)
 {
-    __shared__ ListLds<GIVEN_MOST> l;
-    const int64_t id = grid_row(), r = id / pieces;
+    const int64_t chunks = (classes + v - 1) / v + 1;  // one more than the row has: they are counted from an aligned address in front of it
+    const int block = chunks <= 4 * 64 ? 64 : 256;
+    return {block, (int)((chunks + 4 * block - 1) / (4 * block)), 4 * block};
+}
+
+// ONE: at most one target a row, which is added where its chunk is written; else the targets are a list.
+template <typename T, int BLOCK, bool ONE>
+__global__ __launch_bounds__(BLOCK) void logprob_backward_kernel(const T *logits, int64_t ld, int64_t rows, int n, Pieces pieces, float c, float inv_t,
+                                                                 const int64_t *__restrict__ targets, int given, const float *__restrict__ dlogprob,
+                                                                 const float *__restrict__ dentropy, const float *__restrict__ entropy, const float *__restrict__ stats,
+                                                                 T *out, int64_t ld_out)
+{
+    constexpr int V = CHUNK<T>;
+    __shared__ ListLds<ONE ? 1 : GIVEN_MOST> l;
+    const int64_t id = grid_row(), r = id / pieces.count;
     if (r >= rows) return;
-    const int64_t c0 = (id % pieces) * GRAD_CHUNKS, c1 = c0 + GRAD_CHUNKS;
+    const int64_t c0 = (id % pieces.count) * pieces.chunks, c1 = c0 + pieces.chunks;
     const T *in = logits + r * ld;
     T *to = out + r * ld_out;
     const float m = stats[2 * r], s = stats[2 * r + 1];
     const bool none = m == -INFINITY && s == 0.f;
-    for (int i = threadIdx.x; i < given; i += GRAD_BLOCK) {
-        const int64_t at = targets[r * given + i];
-        l.at[i] = at;
-        l.add[i] = at < 0 || none ? 0.f : at < n ? dlogprob[r * given + i] * inv_t : NAN;
-    }
-    __syncthreads();
+    int64_t target = -1;
     float all = 0.f;
-    for (int i = 0; i < given; ++i) all += l.add[i];
+    auto gradient = [&](int64_t at, float d) { return at < 0 || none ? 0.f : at < n ? d * inv_t : NAN; };
+    if (ONE) {
+        if (given > 0) {
+            target = targets[r];
+            all = gradient(target, dlogprob[r]);
+        }
+    } else {
+        for (int i = threadIdx.x; i < given; i += BLOCK) {
+            l.at[i] = targets[r * given + i];
+            l.add[i] = gradient(l.at[i], dlogprob[r * given + i]);
+        }
+        __syncthreads();
+        for (int i = 0; i < given; ++i) all += l.add[i];
+    }
     // d x = 1/T [ sum dlp (delta - p) - dH p (ln p + H) ] = listed + p (a + b z),  ln p = ln2 z - ln s
     const float dh = dentropy != nullptr ? dentropy[r] * inv_t : 0.f, lns = logf(s);
     const float h = dentropy != nullptr ? entropy[r] : 0.f;
     const float inv_s = none ? 0.f : 1.f / s, a = none ? 0.f : (-all - dh * (h - lns)) * inv_s, b = none ? 0.f : -dh * LN2 * inv_s, m0 = none ? 0.f : m;
     auto value = [&](float x) {
         const float z = fmaxf((x - m0) * c, Z_LEAST);
-        return exp2_fast(z) * (a + b * z);
+        return exp2_fast(z) * fmaf(b, z, a);
     };
-    ListedOut<T, GRAD_BLOCK, GIVEN_MOST> listed;
+    if (ONE) {
+        const int at0 = target >= 0 && target < n ? (int)target : -V;
+        write_row<T, BLOCK, 4>(in, to, n, c0, c1, value, [&](int at, float(&x)[V]) {
+            if ((unsigned)(at0 - at) < (unsigned)V)
+#pragma unroll
+                for (int j = 0; j < V; ++j) x[j] += at + j == at0 ? all : 0.f;
+        });
+        return;
+    }
+    ListedOut<T, BLOCK, ONE ? 1 : GIVEN_MOST> listed;
     listed.read(in, to, n, c0, c1, l, given);
     __syncthreads();
-    write_row<T, GRAD_BLOCK>(in, to, n, c0, c1, value);
+    write_row<T, BLOCK, 4>(in, to, n, c0, c1, value, [](int, float(&)[V]) {});
     __syncthreads();
     listed.write(to, l, given, value);
 }
@@ -651,10 +691,14 @@ __global__ __launch_bounds__(GRAD_BLOCK) void logprob_backward_kernel(const T *l
 template <typename T> static int logprob_backward(const LogitsArgs &a, const int64_t *targets, int given, const float *dlogprob, const float *dentropy, const float *entropy,
                                                   const float *stats, T *out, int64_t ld_out, hipStream_t s)
 {
-    // one chunk more than the row has: its chunks are counted from an aligned address in front of it
-    const int pieces = (int)(((a.classes + CHUNK<T> - 1) / CHUNK<T> + 1 + GRAD_CHUNKS - 1) / GRAD_CHUNKS);
-    hipLaunchKernelGGL(logprob_backward_kernel<T>, row_grid(a.rows * pieces), dim3(GRAD_BLOCK), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces,
-                       LOG2E / a.temperature, 1.f / a.temperature, targets, given, dlogprob, dentropy, entropy, stats, out, ld_out);
+    const Pieces pieces = grad_pieces(a.classes, CHUNK<T>);
+#define OMNI_LOGPROB_BACKWARD(B, ONE)                                                                                                                                           \
+    hipLaunchKernelGGL((logprob_backward_kernel<T, B, ONE>), row_grid(a.rows * pieces.count), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, LOG2E / a.temperature, \
+                       1.f / a.temperature, targets, given, dlogprob, dentropy, entropy, stats, out, ld_out)
+    if (given <= 1 && pieces.block == 64) OMNI_LOGPROB_BACKWARD(64, true);
+    else if (given <= 1) OMNI_LOGPROB_BACKWARD(256, true);
+    else OMNI_LOGPROB_BACKWARD(256, false);
+#undef OMNI_LOGPROB_BACKWARD
     OMNI_LAUNCH_CHECK();
     return OMNI_OK;
 }
@@ -871,16 +915,18 @@ __global__ __launch_bounds__(BLOCK) void distill_loss_kernel(const T *__restrict
     write_loss<T, BLOCK, ALSO>(d, row, r, n, a, loss, stats, l, lds);
 }
 
-// ... of rows whose sums the parts' launch has taken
+// ... of rows whose sums the parts' launch has taken, by as many threads as the gradient's workgroups have there
+constexpr int JOIN_BLOCK = 256;
+
 template <typename T, int ALSO>
-__global__ __launch_bounds__(GRAD_BLOCK) void distill_join_kernel(const T *__restrict__ logits, int64_t ld, int n, int parts, DistillArgs d, float c, const float4 *__restrict__ sums,
+__global__ __launch_bounds__(JOIN_BLOCK) void distill_join_kernel(const T *__restrict__ logits, int64_t ld, int n, int parts, DistillArgs d, float c, const float4 *__restrict__ sums,
                                                           float *__restrict__ loss, float *__restrict__ stats)
 {
-    __shared__ float lds[2 * (GRAD_BLOCK / 64)];
+    __shared__ float lds[2 * (JOIN_BLOCK / 64)];
     __shared__ EntryLds l;
     const int64_t r = blockIdx.x;
     const Sums a = join_parts<ALSO>(sums + r * parts, parts, c);
-    write_loss<T, GRAD_BLOCK, ALSO>(d, logits + r * ld, r, n, a, loss, stats, l, lds);
+    write_loss<T, JOIN_BLOCK, ALSO>(d, logits + r * ld, r, n, a, loss, stats, l, lds);
 }
 
 // Loss and gradient of whole rows.  The row's first KEPT chunks a thread stay in registers from the sums to the gradient; what
@@ -927,34 +973,35 @@ __global__ __launch_bounds__(BLOCK) void distill_both_kernel(const T *logits, in
 
 // The gradient from given sums: the statistics of an earlier call, or (sums != null) the parts' of this one.  loss != null: the
 // row's first workgroup writes the loss, too, for which it reads all over the row -- not where the row is overwritten.
-template <typename T, int ALSO>
-__global__ __launch_bounds__(GRAD_BLOCK) void distill_backward_kernel(const T *logits, int64_t ld, int64_t rows, int n, int pieces, DistillArgs d, float c,
+template <typename T, int BLOCK, int ALSO>
+__global__ __launch_bounds__(BLOCK) void distill_backward_kernel(const T *logits, int64_t ld, int64_t rows, int n, Pieces pieces, DistillArgs d, float c,
                                                                       const float *__restrict__ stats, const float4 *__restrict__ sums, int parts, float *__restrict__ loss,
                                                                       T *out, int64_t ld_out)
 {
-    __shared__ float lds[2 * (GRAD_BLOCK / 64)];
+    __shared__ float lds[2 * (BLOCK / 64)];
     __shared__ EntryLds l;
-    const int64_t id = grid_row(), r = id / pieces;
+    const int64_t id = grid_row(), r = id / pieces.count;
     if (r >= rows) return;
-    const int64_t c0 = (id % pieces) * GRAD_CHUNKS, c1 = c0 + GRAD_CHUNKS;
+    const int64_t c0 = (id % pieces.count) * pieces.chunks, c1 = c0 + pieces.chunks;
     const T *in = logits + r * ld;
     T *to = out + r * ld_out;
     Sums a;
     if (sums != nullptr) a = join_parts<ALSO>(sums + r * parts, parts, c);
     else a = {stats[4 * r], 0.f, stats[4 * r + 1], stats[4 * r + 2]};
-    const Entries e = read_entries<GRAD_BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
+    const Entries e = read_entries<BLOCK>(d, r, n, 1.f / d.temperature, l, lds);
     __syncthreads();
     if (loss != nullptr && c0 == 0) {
-        const float v = row_loss<T, GRAD_BLOCK, ALSO != NOTHING>(d, in, r, n, a, e, l, lds);
+        const float v = row_loss<T, BLOCK, ALSO != NOTHING>(d, in, r, n, a, e, l, lds);
         if (threadIdx.x == 0) loss[r] = v;
         __syncthreads();
     }
-    const Coefs k = row_coefs<GRAD_BLOCK, ALSO != NOTHING>(d, r, n, a.m, a.s, a.t, e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
+    const Coefs k = row_coefs<BLOCK, ALSO != NOTHING>(d, r, n, a.m, a.s, a.t, e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
     const Gradient<ALSO> value(k, a.m, c);
-    ListedOut<T, GRAD_BLOCK, KEPT_MOST + 1> listed;
+    ListedOut<T, BLOCK, KEPT_MOST + 1> listed;
     listed.read(in, to, n, c0, c1, l, k.count);
     __syncthreads();
-    write_row<T, GRAD_BLOCK>(in, to, n, c0, c1, value);
+    // (2048 x 65536 fp32: 196 us with one chunk ahead, 212 with four; 4096 x 65536 bf16: 197 and 180)
+    write_row<T, BLOCK, sizeof(T) == 4 ? 1 : 4>(in, to, n, c0, c1, value, [](int, float(&)[CHUNK<T>]) {});
     __syncthreads();
     listed.write(to, l, k.count, value);
 }
@@ -989,7 +1036,7 @@ template <typename T> static int distill_loss(const LogitsArgs &a, const Distill
 #define OMNI_DISTILL_PARTS(UNUSED, ALSO)                                                                                                                                 \
     do {                                                                                                                                                                 \
         if ((st = launch_parts<T, ALSO>(a, p, c, 0, sums, nullptr, s)) != OMNI_OK) return st;                                                                            \
-        hipLaunchKernelGGL((distill_join_kernel<T, ALSO>), dim3((unsigned)a.rows), dim3(GRAD_BLOCK), 0, s, (const T *)a.logits, a.ld, (int)a.classes, p.count, d, c, sums, loss, stats); \
+        hipLaunchKernelGGL((distill_join_kernel<T, ALSO>), dim3((unsigned)a.rows), dim3(JOIN_BLOCK), 0, s, (const T *)a.logits, a.ld, (int)a.classes, p.count, d, c, sums, loss, stats); \
     } while (0)
         OMNI_BY_SECOND(OMNI_DISTILL_PARTS, 0);
 #undef OMNI_DISTILL_PARTS
@@ -1015,11 +1062,12 @@ template <typename T>
 static int distill_backward(const LogitsArgs &a, const DistillArgs &d, const float *stats, const float4 *sums, int parts, float *loss, T *out, int64_t ld_out, hipStream_t s)
 {
     const float c = distill_scale(d);
-    const int pieces = (int)(((a.classes + CHUNK<T> - 1) / CHUNK<T> + 1 + GRAD_CHUNKS - 1) / GRAD_CHUNKS);
+    const Pieces pieces = grad_pieces(a.classes, CHUNK<T>);
 #define OMNI_DISTILL_BACKWARD(B, ALSO)                                                                                                                              \
-    hipLaunchKernelGGL((distill_backward_kernel<T, ALSO>), row_grid(a.rows * pieces), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, d, c, stats, \
+    hipLaunchKernelGGL((distill_backward_kernel<T, B, ALSO>), row_grid(a.rows * pieces.count), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, d, c, stats, \
                        sums, parts, loss, out, ld_out)
-    OMNI_BY_SECOND(OMNI_DISTILL_BACKWARD, GRAD_BLOCK);
+    if (pieces.block == 64) OMNI_BY_SECOND(OMNI_DISTILL_BACKWARD, 64);
+    else OMNI_BY_SECOND(OMNI_DISTILL_BACKWARD, JOIN_BLOCK);
 #undef OMNI_DISTILL_BACKWARD
     OMNI_LAUNCH_CHECK();
     return OMNI_OK;
@@ -1038,7 +1086,7 @@ template <typename T> static int distill_both(const LogitsArgs &a, const Distill
     do {                                                                                                                                                                 \
         if ((st = launch_parts<T, ALSO>(a, p, c, 0, sums, nullptr, s)) != OMNI_OK) return st;                                                                            \
         if (over)                                                                                                                                                        \
-            hipLaunchKernelGGL((distill_join_kernel<T, ALSO>), dim3((unsigned)a.rows), dim3(GRAD_BLOCK), 0, s, (const T *)a.logits, a.ld, (int)a.classes, p.count, d, c, sums,   \
+            hipLaunchKernelGGL((distill_join_kernel<T, ALSO>), dim3((unsigned)a.rows), dim3(JOIN_BLOCK), 0, s, (const T *)a.logits, a.ld, (int)a.classes, p.count, d, c, sums,   \
                                loss, nullptr);                                                                                                                           \
     } while (0)
         OMNI_BY_SECOND(OMNI_DISTILL_PARTS, 0);
