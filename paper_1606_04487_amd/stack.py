@@ -2,8 +2,9 @@
 
 This is the thin harness the tests and the bench use for the paper's CIFAR-style and
 CaffeNet-style convolution phases (Sec. II-C: the "conv phase" of a CNN; Sec. IV-A: an engine is
-a list of layers run forward and then in reverse).  It only sequences calls of the binding and
-owns the device buffers; every arithmetic step runs in the library's kernels.
+a list of layers run forward and then in reverse), the loss behind it (`distill_step`) and what
+is read off its answers (`log_probs`).  It only sequences calls of the binding and owns the device
+buffers; every arithmetic step runs in the library's kernels.
 
 Memory plan (sized for one MI355X's 288 GB): every layer keeps its own forward workspace, so the
 lowered matrix D-hat written by the forward pass is still there when the backward pass needs it
@@ -18,6 +19,27 @@ import torch
 
 from . import binding as B
 from .workloads import ConvLayer
+
+
+class _Norm:
+    """Layer norm over all of an image's values behind a layer whose output is `out`: weights, their velocities and gradients, and
+    the buffers of its two passes."""
+
+    def __init__(self, out: torch.Tensor, device: str):
+        N, width = out.shape[0], out.numel() // out.shape[0]
+        self.gamma, self.beta, self.vgamma, self.vbeta, self.dgamma, self.dbeta = (
+            torch.zeros((width,), dtype=torch.float32, device=device) for _ in range(6))
+        self.y, self.dx = (torch.empty((N, width), dtype=out.dtype, device=device) for _ in range(2))
+        self.mean, self.rstd = (torch.empty((N,), dtype=torch.float32, device=device) for _ in range(2))
+        need = B.layer_norm_workspace_bytes(N, width, out.dtype)
+        self.workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        self.x: Optional[torch.Tensor] = None
+        self.reset()
+
+    def reset(self) -> None:
+        self.gamma.fill_(1.0)
+        for t in (self.beta, self.vgamma, self.vbeta):
+            t.zero_()
 
 
 class ConvStack:
@@ -82,6 +104,7 @@ class ConvStack:
         # is by both backward passes of the convolution, instead of a dense tensor that the library would repack
         self.dYr, self.dYs, self.rows_ld = [], [], []
         self.Nrm, self.Sc, self.Dr, self.gN, self.gD = [], [], [], [], []   # normalised / scale / dropped; their gradients
+        self.norms: List[Optional[_Norm]] = []
         for i, (L, d) in enumerate(zip(self.layers, self.desc)):
             ho, wo = B.conv_output_dims(d)
             self.Y.append(torch.empty((L.N, L.F, ho, wo), dtype=self.tdtype, device=device))
@@ -107,7 +130,10 @@ class ConvStack:
             self.gN.append(torch.empty_like(out) if L.lrn_after else None)
             self.Dr.append(torch.empty_like(out) if L.dropout_after > 0 else None)
             self.gD.append(torch.empty_like(out) if L.dropout_after > 0 else None)
+            self.norms.append(_Norm(out, device) if L.norm_after else None)
             self.dXl.append(torch.empty((L.N, L.C, L.H, L.W), dtype=self.tdtype, device=device) if need_dx else None)
+        self.d_logits: Optional[torch.Tensor] = None   # distill_step's
+        self.loss: Optional[torch.Tensor] = None
         # A convolution + ReLU layer directly in front of another rows-form layer: that layer's data gradient applies
         # the ReLU's mask and stores the result as this layer's rows matrix itself (with partial sums per column
         # tile instead of per plane), so neither a dense dX nor a separate ReLU backward pass exists for the pair.
@@ -115,7 +141,7 @@ class ConvStack:
         for i in range(len(self.layers) - 1):
             L = self.layers[i]
             if not (fuse_relu_dgrad and self.dYr[i] is not None and self.dYr[i + 1] is not None and L.relu
-                    and not L.pool_after and not L.lrn_after and L.dropout_after == 0):
+                    and not L.pool_after and not L.lrn_after and not L.norm_after and L.dropout_after == 0):
                 continue
             per = B.conv_backward_data_relu_rows_sums(self.desc[i + 1])
             if per is None:
@@ -146,6 +172,9 @@ class ConvStack:
                 self.Wc[i].copy_(self.W[i])       # plumbing: the inputs are bf16-representable already
             self.VW[i].zero_()
             self.Vb[i].zero_()
+        for m in self.norms:
+            if m is not None:
+                m.reset()
         self.repack_weights()
 
     def repack_weights(self) -> None:
@@ -160,10 +189,12 @@ class ConvStack:
         last = self.P[-1] if self.P[-1] is not None else self.Y[-1]
         return tuple(last.shape)
 
+    NORM_EPS = 1e-5              # layer norm's
     LRN = (5, 1e-4, 0.75, 1.0)   # channel window, alpha, beta, k of the network's normalisation layers
 
     # ------------------------------------------------------------------ passes
-    def forward(self, X: torch.Tensor) -> torch.Tensor:
+    def forward(self, X: torch.Tensor, train: bool = True) -> torch.Tensor:
+        """The output for X.  train = False leaves the dropout layers out."""
         cur = X
         for i, L in enumerate(self.layers):
             self.X[i] = cur
@@ -178,7 +209,12 @@ class ConvStack:
             if L.lrn_after:
                 B.lrn_forward(cur, *self.LRN, y=self.Nrm[i], scale=self.Sc[i])
                 cur = self.Nrm[i]
-            if L.dropout_after > 0:
+            if L.norm_after:
+                m = self.norms[i]
+                B.layer_norm_forward(cur.view(L.N, -1), m.gamma, m.beta, self.NORM_EPS, m.y, m.mean, m.rstd)
+                m.x = cur
+                cur = m.y.view(cur.shape)
+            if train and L.dropout_after > 0:
                 B.dropout_forward(cur, L.dropout_after, self.dropout_seed, i, y=self.Dr[i])
                 cur = self.Dr[i]
         return cur
@@ -190,6 +226,11 @@ class ConvStack:
             if L.dropout_after > 0:
                 B.dropout_backward(g, L.dropout_after, self.dropout_seed, i, dx=self.gD[i])
                 g = self.gD[i]
+            if L.norm_after:
+                m = self.norms[i]
+                B.layer_norm_backward(m.x.view(L.N, -1), g.view(L.N, -1), m.mean, m.rstd, m.gamma, m.dx, m.dgamma, m.dbeta,
+                                      workspace=m.workspace)
+                g = m.dx.view(g.shape)
             if L.lrn_after:
                 B.lrn_backward(self.P[i] if L.pool_after else Y, g, self.Sc[i], *self.LRN, dx=self.gN[i])
                 g = self.gN[i]
@@ -244,10 +285,13 @@ class ConvStack:
         return g
 
     def sgd_step(self, lr: float, momentum: float, weight_decay: float = 0.0) -> None:
+        norms = [m for m in self.norms if m is not None]
         shadow = None
         if self.dtype == B.BF16:
-            shadow = list(self.Wc) + [None] * len(self.b)
-        B.sgd_momentum_step(self.W + self.b, self.VW + self.Vb, self.dW + self.db, lr, momentum,
+            shadow = list(self.Wc) + [None] * (len(self.b) + 2 * len(norms))
+        B.sgd_momentum_step(self.W + self.b + [p for m in norms for p in (m.gamma, m.beta)],
+                            self.VW + self.Vb + [v for m in norms for v in (m.vgamma, m.vbeta)],
+                            self.dW + self.db + [d for m in norms for d in (m.dgamma, m.dbeta)], lr, momentum,
                             weight_decay, shadow)
         self.repack_weights()
 
@@ -258,6 +302,32 @@ class ConvStack:
         self.sgd_step(lr, momentum, weight_decay)
         return out
 
+    # ------------------------------------------------------------------ the end of the network
+    def logits(self, out: torch.Tensor) -> torch.Tensor:
+        """The output as a matrix [N][classes]."""
+        return out.view(out.shape[0], -1)
+
+    def log_probs(self, X: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 5, temperature: float = 1.0):
+        """What the network answers for X (without dropout): (logprob, entropy, top_index, top_logprob) of
+        binding.logprob_forward.  The top alternatives are what distill_step takes of a teacher."""
+        return B.logprob_forward(self.logits(self.forward(X, train=False)), targets, top, temperature, want_stats=False)[:4]
+
+    def distill_step(self, X: torch.Tensor, teacher_index: Optional[torch.Tensor], teacher_logits: Optional[torch.Tensor],
+                     labels: Optional[torch.Tensor], lr: float, momentum: float, weight_decay: float = 0.0, temperature: float = 1.0,
+                     alpha: float = 1.0) -> torch.Tensor:
+        """One training step on the mean over the batch of the distillation loss (binding.distill_forward; alpha = 0 and no teacher:
+        the labels' cross entropy): forward, loss and its gradient, backward, update.  Returns the loss of every image."""
+        logits = self.logits(self.forward(X))
+        N = logits.shape[0]
+        if self.d_logits is None:
+            self.d_logits = torch.empty_like(logits)
+            self.loss = torch.empty((N,), dtype=torch.float32, device=logits.device)
+        B.distill_forward_backward(logits, teacher_index, teacher_logits, labels, temperature, alpha, scale=1.0 / N, loss=self.loss,
+                                   dlogits=self.d_logits)
+        self.backward(self.d_logits.view(self.output_shape()))
+        self.sgd_step(lr, momentum, weight_decay)
+        return self.loss
+
     # ------------------------------------------------------------------ state checks (plumbing, after a run)
     def tensor_health(self, W_start: Optional[Sequence[torch.Tensor]] = None) -> dict:
         """Finiteness and spread of the tensors the last step left: parameters, velocities, gradients, every
@@ -265,6 +335,7 @@ class ConvStack:
         torch.cuda.synchronize()
         last_dx = next((d for d in self.dXl if d is not None), None)
         state = list(self.W) + list(self.b) + list(self.VW) + list(self.Vb) + list(self.dW) + list(self.db) + list(self.Y)
+        state += [t for m in self.norms if m is not None for t in (m.gamma, m.beta, m.vgamma, m.vbeta, m.dgamma, m.dbeta)]
         if last_dx is not None:
             state.append(last_dx)
         h = {

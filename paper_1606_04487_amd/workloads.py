@@ -33,6 +33,7 @@ class ConvLayer:
     relu: bool = True             # ReLU on the layer's output (the last fully connected layer has none)
     lrn_after: bool = False       # normalisation across 5 channels follows the pool (alpha 1e-4, beta 0.75, k 1)
     dropout_after: float = 0.0    # drop probability of a dropout layer that follows (0: none)
+    norm_after: bool = False      # layer norm over all of an image's values follows, in front of the dropout
 
     @property
     def Ho(self) -> int:
@@ -98,16 +99,17 @@ def step_upstream_scale(N: int) -> float:
     return 2.0 ** -(18 + max(0, math.ceil(math.log2(N))))
 
 
-def caffenet_full(N: int = 256) -> List[ConvLayer]:
+def caffenet_full(N: int = 256, norm: bool = False) -> List[ConvLayer]:
     """The whole CaffeNet-shaped network (Sec. II-C: conv phase, then FC phase): conv1..conv5 as above with the
     two normalisation layers after the first two pools, then FC6 (the convolution whose 6 x 6 window covers the
-    whole 256 x 6 x 6 image), FC7 and FC8 (1 x 1 convolutions on 1 x 1 images), dropout 0.5 after FC6 and FC7."""
+    whole 256 x 6 x 6 image), FC7 and FC8 (1 x 1 convolutions on 1 x 1 images), dropout 0.5 after FC6 and FC7.
+    norm: layer norm after the ReLUs of FC6 and FC7 as well (no part of the paper's network)."""
     conv = caffenet_stack(N)
     conv[0] = replace(conv[0], lrn_after=True)
     conv[1] = replace(conv[1], lrn_after=True)
     return conv + [
-        ConvLayer("fc6", N, 256, 6, 6, 4096, 6, 1, 0, dropout_after=0.5),
-        ConvLayer("fc7", N, 4096, 1, 1, 4096, 1, 1, 0, dropout_after=0.5),
+        ConvLayer("fc6", N, 256, 6, 6, 4096, 6, 1, 0, dropout_after=0.5, norm_after=norm),
+        ConvLayer("fc7", N, 4096, 1, 1, 4096, 1, 1, 0, dropout_after=0.5, norm_after=norm),
         ConvLayer("fc8", N, 4096, 1, 1, 1000, 1, 1, 0, relu=False),
     ]
 
