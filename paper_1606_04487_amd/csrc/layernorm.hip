@@ -245,9 +245,9 @@ template <int TILE, typename T> __device__ __forceinline__ void norm_columns(con
 
 // Tiles of 8 chunks, 128 bytes of a row and so a cache line, where there are enough of them to occupy the chip, else of 4.
 constexpr int LN_TILE = 8, LN_NARROW = 4, LN_LDS = 16 * 2 * 8 * LN_TILE;
-template <typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, float *lds)
+template <typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, int id, float *lds)
 {
-    const int tile = (int)blockIdx.x % a.tiles, which = (int)blockIdx.x / a.tiles;
+    const int tile = id % a.tiles, which = id / a.tiles;
     if (a.narrow) norm_columns<LN_NARROW>(a, tile, which, lds);
     else norm_columns<LN_TILE>(a, tile, which, lds);
 }
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(4, 4))) vo
     __shared__ float lds[2][2][16];
     __shared__ float sums[WEIGHTS ? 1 : LN_LDS];
     if (!WEIGHTS && (int)blockIdx.x < columns) {
-        norm_columns(a, sums);
+        norm_columns(a, blockIdx.x, sums);
         return;
     }
     const int team = threadIdx.x / TEAM, lane = threadIdx.x % TEAM;
@@ -372,17 +372,18 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(4, 4))) vo
 }
 
 // Rows of more chunks than that: the first LONG_KEPT chunks a thread of x and dy are kept as they lie in memory, what is beyond
-// them is read a second time from the caches.
+// them is read a second time from the caches.  (2^28 columns are 2^22 tiles of bf16, 2^23 of fp32: more than a grid's x takes.)
 template <typename T> __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(NormBackward<T> a, int columns)
 {
     constexpr int V = CHUNK<T>, STEP = 1024 * V, KEPT = LONG_KEPT / 2;
     __shared__ float lds[2][16];
     __shared__ float sums[LN_LDS];
-    if ((int)blockIdx.x < columns) {
-        norm_columns(a, sums);
+    const int64_t id = grid_row(), r = id - columns;
+    if (id < columns) {
+        norm_columns(a, (int)id, sums);
         return;
     }
-    const int64_t r = blockIdx.x - columns;
+    if (a.dx == nullptr || r >= a.rows) return;
     const T *xr = a.x + r * a.ldx, *dr = a.dy + r * a.lddy;
     const float mu = a.mean[r], rs = a.rstd[r];
     const int first = threadIdx.x * V;
@@ -542,7 +543,7 @@ template <typename T> static int backward_launch(const NormBackward<T> &b, bool 
     else if (chunks <= 512) launch_backward<T, 512, 1>(b, fused, columns, parts, dx, s);
     else if (chunks <= 1024) launch_backward<T, 1024, 1>(b, fused, columns, parts, dx, s);
     else if (chunks <= 2048) launch_backward<T, 1024, 2>(b, fused, columns, parts, dx, s);
-    else hipLaunchKernelGGL(layer_norm_backward_long_kernel<T>, dim3((unsigned)(columns + (dx ? b.rows : 0))), dim3(1024), 0, s, b, (int)columns);
+    else hipLaunchKernelGGL(layer_norm_backward_long_kernel<T>, row_grid(columns + (dx ? b.rows : 0)), dim3(1024), 0, s, b, (int)columns);
     OMNI_LAUNCH_CHECK();
     return OMNI_OK;
 }
@@ -553,7 +554,7 @@ static int backward(const LayerNormArgs &a, const T *dy, int64_t lddy, const flo
 {
     const bool weights = dgamma != nullptr || dbeta != nullptr;
     WeightsPlan p = weights_plan(a.dtype, a.rows, a.width);
-    const int64_t range = p.fused || p.parts == 0 ? a.rows : (a.rows + p.parts - 1) / p.parts, columns = p.tiles * p.parts;
+    const int64_t range = p.fused ? a.rows : (a.rows + p.parts - 1) / p.parts, columns = p.tiles * p.parts;
     NormBackward<T> b = {(const T *)a.x, dy, a.ldx, lddy, a.rows, (int)a.width, a.gamma, mean, rstd, dx, lddx, dgamma, dbeta, p.parts > 1 ? part : nullptr, (int)p.tiles, p.narrow ? 1 : 0, range};
     int st;
     if (!weights) {  // (the resident workgroups are the faster ones for many rows, also without sums to leave)

@@ -198,3 +198,49 @@ def test_other_stream_and_a_replayed_graph(B):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, (out["y"], out["dx"], dg, db)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_widest_row(B, dtype):
+    # 2^28 columns, whose tiles are more than one grid dimension takes.  x = +-1 and eps = 0: xh = x exactly, dy = 0, 1, 2, 3, 0, ...:
+    # mean dy = 3/2 and mean dy xh = -1/2, and every partial sum is a whole number a thread can hold, so nothing is rounded.
+    n = 1 << 28
+    x = torch.tensor([1.0, -1.0], device="cuda", dtype=dtype).repeat(n // 2).view(1, n)
+    dy = torch.tensor([0.0, 1.0, 2.0, 3.0], device="cuda", dtype=dtype).repeat(n // 4).view(1, n)
+    y, mean, rstd = B.layer_norm_forward(x, eps=0.0)
+    assert torch.equal(y, x) and mean.item() == 0.0 and rstd.item() == 1.0
+    dx, dg, db = B.layer_norm_backward(x, dy, mean, rstd)
+    assert torch.equal(db, dy.view(-1).float())
+    assert torch.equal(dg.view(-1, 4), torch.tensor([0.0, -1.0, 2.0, -3.0], device="cuda").expand(n // 4, 4))
+    assert torch.equal(dx.view(-1, 4), torch.tensor([-1.0, -1.0, 1.0, 1.0], device="cuda", dtype=dtype).expand(n // 4, 4))
+    del x, dy, y, dx, dg, db
+    torch.cuda.empty_cache()
+
+
+def test_rows_of_three_dimensions_and_what_is_refused(B):
+    base = torch.randn(3, 8, 40, device="cuda")
+    x = base[:, ::2, :33]  # 12 rows, 80 apart
+    gamma = torch.randn(33, device="cuda")
+    y, mean, rstd = B.layer_norm_forward(x, gamma)
+    want = B.layer_norm_forward(x.contiguous().view(12, 33), gamma)
+    assert y.shape == x.shape and mean.shape == x.shape[:-1] and torch.equal(y.view(12, 33), want[0]) and torch.equal(rstd.view(-1), want[2])
+    got = B.layer_norm_backward(x, y, mean, rstd, gamma)
+    wanted = B.layer_norm_backward(x.contiguous().view(12, 33), y.view(12, 33), want[1], want[2], gamma)
+    assert got[0].shape == x.shape and all(torch.equal(a.reshape(b.shape), b) for a, b in zip(got, wanted))
+    one = torch.randn(33, device="cuda")
+    assert torch.equal(B.layer_norm_forward(one)[0], B.layer_norm_forward(one.view(1, 33))[0][0])
+    for bad in (base[:, :5, :33],                       # rows that are not evenly spaced
+                base.transpose(1, 2),                   # rows that are not contiguous
+                torch.randn(1, 33, device="cuda").expand(4, 33),  # one row four times
+                torch.randn(70, device="cuda").as_strided((3, 33), (10, 1)),
+                torch.empty(4, 0, device="cuda"), torch.tensor(1.0, device="cuda"), torch.zeros(4, 33, device="cuda", dtype=torch.int32)):
+        with pytest.raises((ValueError, TypeError, B.OmniError)):
+            B.layer_norm_forward(bad)
+    for kw in (dict(gamma=gamma[:32]), dict(gamma=gamma.double()), dict(gamma=gamma.cpu()), dict(y=torch.empty(11, 33, device="cuda")),
+               dict(y=torch.empty(12, 33, device="cuda", dtype=torch.bfloat16)), dict(mean=torch.empty(11, device="cuda")), dict(eps=-1.0)):
+        with pytest.raises((ValueError, B.OmniError)):
+            B.layer_norm_forward(x, **kw)
+    many = torch.zeros(4099, 130, device="cuda")
+    rows = torch.zeros(4099, device="cuda")
+    with pytest.raises((ValueError, B.OmniError)):
+        B.layer_norm_backward(many, many, rows, rows, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
