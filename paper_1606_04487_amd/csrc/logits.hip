@@ -239,13 +239,13 @@ constexpr int TOP_KEYS = 512, TOP_LIST = 256;
 template <int BLOCK> struct TopLds {
     uint64_t keys[TOP_KEYS];
     uint64_t bar;
-    uint32_t group[256];
+    uint32_t group[BLOCK];
     int count, listed;
-    uint16_t list[TOP_LIST];  // slot * 1024 + thread
+    uint16_t list[TOP_LIST];  // slot * BLOCK + thread
 };
 
-// The k largest of a row, k <= 64, in order.  The k-th largest of the maxima of 256 groups of threads (of single chunks, in a
-// workgroup of one wavefront) is a lower bound of the k-th largest element; the elements that reach it are collected, few more
+// The k largest of a row, k <= 64, in order, by a workgroup of 64 or 256.  The k-th largest of the threads' maxima (of single
+// chunks', by one wavefront for k > 16) is a lower bound of the k-th largest element; the elements that reach it are collected, few more
 // than k, and ranked by comparing each with all.  A row that the threads keep (KEPT > 0) is looked through where it lies; of others
 // only the slots whose maximum reaches the bound are read again, their chunks spread over the workgroup (every chunk of the
 // threads that reach it instead: 149 us for 32 of 2048 x 131072 bf16, where the sums alone take 85: the chunks of one thread lie
@@ -256,6 +256,7 @@ template <typename T, int BLOCK, int KEPT, typename PUT>
 __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &sp, float own, int k, TopLds<BLOCK> &t, const uint4 (&kept)[KEPT > 0 ? KEPT : 1],
                                         const Slots<BLOCK> *slots, int shift, PUT put)
 {
+    static_assert(BLOCK == 256 || (BLOCK == 64 && KEPT > 0), "groups of a lane");
     constexpr int V = CHUNK<T>, EACH = BLOCK == 64 ? KEPT : 4;  // groups that a lane compares
     const int tid = threadIdx.x, lane = tid & 63, rest = KEPT > 0 ? sp.hi : sp.lo;
     uint32_t u[EACH], bound = 0;
@@ -272,13 +273,8 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
             for (int j = 0; j < V; ++j) g = sp.lo + tid + i * 64 < sp.hi ? fmaxf(g, x[j]) : g;
             u[i] = ordered(fmaxf(g, -INFINITY));
         }
-    } else {
-        float g = own;
-        if (BLOCK == 1024) {
-            g = fmaxf(g, dpp<0xb1>(g));
-            g = fmaxf(g, dpp<0x4e>(g));
-        }
-        if (tid % (BLOCK / 256) == 0) t.group[tid / (BLOCK / 256)] = ordered(g);
+    } else {  // every thread is
+        t.group[tid] = ordered(own);
         if (tid == 0) t.listed = 0;
         __syncthreads();
 #pragma unroll
@@ -301,7 +297,7 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
         for (int i = 0; i << shift < batches; ++i)
             if (slots->most[i][tid] >= bound >> 16) {
                 const int to = atomicAdd(&t.listed, 1);
-                if (to < TOP_LIST) t.list[to] = (uint16_t)(i * 1024 + tid);
+                if (to < TOP_LIST) t.list[to] = (uint16_t)(i * BLOCK + tid);
             }
     uint64_t bar = (uint64_t)bound << 32;
     int found;
@@ -336,7 +332,7 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
         if (listed <= TOP_LIST) {
             const int each = 2 + shift;  // chunks of a slot: BATCH << shift
             for (int i = tid; i < listed << each; i += BLOCK) {
-                const int e = t.list[i >> each], q = i & ((1 << each) - 1), c = rest + (e & 1023) + (((e >> 10) << each) + q) * BLOCK;
+                const int e = t.list[i >> each], q = i & ((1 << each) - 1), c = rest + e % BLOCK + ((e / BLOCK << each) + q) * BLOCK;
                 if (c < sp.hi) offer_chunk(raw_chunk<T, false>(row, sp.first(c)), c);
             }
         } else {

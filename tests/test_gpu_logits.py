@@ -431,3 +431,34 @@ def test_together_on_other_streams_and_in_a_replayed_graph(B):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, outs))
+
+
+def test_widest_row(B):
+    # 2^30 classes of 0 but for three.  A thread of the 64 parts adds 2^16 terms in two chains, so the sum is off by 2^15 + 64
+    # roundings at most, relatively; a gradient by as much and the half step it is stored with.
+    n = 1 << 30
+    x = torch.zeros(1, n, dtype=torch.bfloat16, device="cuda")
+    x[0, 5], x[0, n - 1], x[0, 1 << 29] = 1.0, 2.0, -float("inf")
+    s = (n - 3) * np.exp(-2.0) + np.exp(-1.0) + 1.0
+    slack = (2.0 ** 15 + 64) * U
+    targets = torch.tensor([[n - 1, 5, 1 << 29, 7]], device="cuda")
+    lp, entropy, index, best, stats = B.logprob_forward(x, targets, top=2)
+    ref = np.array([0.0, -1.0, -np.inf, -2.0]) - np.log(s)
+    near(host(lp)[0], ref, slack + 8 * U * np.log(s))
+    assert index.tolist() == [[n - 1, 5]] and np.all(np.abs(host(best)[0] - ref[:2]) <= slack + 8 * U * np.log(s))
+    h = -((n - 3) * np.exp(ref[3]) * ref[3] + np.exp(ref[1]) * ref[1] + np.exp(ref[0]) * ref[0])
+    assert abs(entropy.item() - h) <= 3 * slack * (np.log(s) + 2.0)
+    grad = B.logprob_backward(x, stats, targets[:, :1].contiguous(), torch.ones(1, device="cuda"))
+    p = np.exp(ref)
+    tol = 2 * slack + 2.0 ** -8
+    got = host(grad[0, targets[0]])
+    assert abs(got[0] - (1 - p[0])) <= tol and np.all(np.abs(got[1:] + p[1:]) <= tol * p[1:])
+    grad[0, targets[0]] = grad[0, 8].item()
+    assert bool((grad == grad[0, 8]).all()) and abs(grad[0, 8].item() + p[3]) <= tol * p[3]
+    loss, both = B.distill_forward_backward(x, index, best, temperature=1.0, alpha=1.0, dlogits=grad)
+    q = np.exp(ref[:2]) / np.exp(ref[:2]).sum()
+    assert abs(loss.item() - (q * (np.log(q) - ref[:2])).sum()) <= slack + 16 * U * np.log(s)
+    got = host(both[0, targets[0]])
+    assert np.all(np.abs(got - (p - np.array([q[0], q[1], 0.0, 0.0]))) <= tol * np.array([1.0, 1.0, p[2], p[3]]))
+    del x, grad, both
+    torch.cuda.empty_cache()
