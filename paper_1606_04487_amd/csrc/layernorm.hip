@@ -29,7 +29,7 @@ template <int TEAM, int N> __device__ __forceinline__ void team_join(float (&v)[
 }
 
 // CHUNK floats of a vector over the columns, or `fill`
-template <int V> __device__ __forceinline__ void load_columns(const float *p, int at, int n, float fill, float (&v)[V])
+template <Fit FIT, int V> __device__ __forceinline__ void load_columns(const float *p, int at, int n, float fill, float (&v)[V])
 {
     if (p != nullptr && at + V <= n) {
 #pragma unroll
@@ -39,7 +39,7 @@ template <int V> __device__ __forceinline__ void load_columns(const float *p, in
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = p != nullptr && at + j < n ? p[at + j] : fill;
+        for (int j = 0; j < V; ++j) v[j] = FIT != WHOLE && p != nullptr && at + j < n ? p[at + j] : fill;
     }
 }
 
@@ -48,8 +48,8 @@ template <int V> __device__ __forceinline__ void load_columns(const float *p, in
 // output); a workgroup goes on to further rows with gamma and beta in registers too and the next row's loads in flight, since
 // from the caches the two of them are 8 bytes an element where a bf16 element itself is 4, read and written.
 // The squares are summed about the mean, not as mean x^2 - mu^2, which cancels where |mu| is large against the spread.
-template <typename T, int BLOCK, int CHUNKS, bool CUT>
-__global__ __launch_bounds__(BLOCK, BLOCK <= 512 ? 6 : 4) void layer_norm_forward_kernel(const T *x, int64_t ldx, int64_t rows, int n, float eps, const float *__restrict__ gamma,
+template <typename T, int BLOCK, int CHUNKS, Fit FIT>
+__global__ __launch_bounds__(BLOCK, BLOCK <= 512 ? (FIT == CUT && BLOCK == 512 ? 4 : 6) : 4) void layer_norm_forward_kernel(const T *x, int64_t ldx, int64_t rows, int n, float eps, const float *__restrict__ gamma,
                                                                    const float *__restrict__ beta, T *y, int64_t ldy, float *__restrict__ mean, float *__restrict__ rstd)
 {
     constexpr int V = CHUNK<T>;
@@ -61,21 +61,21 @@ __global__ __launch_bounds__(BLOCK, BLOCK <= 512 ? 6 : 4) void layer_norm_forwar
     if (r >= rows) return;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        next[c] = load_raw(x + r * ldx, (c * BLOCK + tid) * V, n);
-        load_columns<V>(gamma, (c * BLOCK + tid) * V, n, 1.f, ga[c]);
-        load_columns<V>(beta, (c * BLOCK + tid) * V, n, 0.f, be[c]);
+        next[c] = load_raw<FIT>(x + r * ldx, (c * BLOCK + tid) * V, n);
+        load_columns<FIT, V>(gamma, (c * BLOCK + tid) * V, n, 1.f, ga[c]);
+        load_columns<FIT, V>(beta, (c * BLOCK + tid) * V, n, 0.f, be[c]);
     }
     for (;;) {
         float v[CHUNKS][V], sum[1] = {0.f}, sq[1] = {0.f};
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            settle<CUT>(next[c], (c * BLOCK + tid) * V, n);
+            settle<FIT>(next[c], (c * BLOCK + tid) * V, n);
             unpack(next[c].w, v[c]);
         }
         const int64_t r2 = r + (int64_t)gridDim.x * gridDim.y;
         if (r2 < rows)
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) next[c] = load_raw(x + r2 * ldx, (c * BLOCK + tid) * V, n);
+            for (int c = 0; c < CHUNKS; ++c) next[c] = load_raw<FIT>(x + r2 * ldx, (c * BLOCK + tid) * V, n);
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
@@ -89,9 +89,9 @@ __global__ __launch_bounds__(BLOCK, BLOCK <= 512 ? 6 : 4) void layer_norm_forwar
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 v[c][j] -= mu;
-                if (!CUT || at + j < n) q += v[c][j] * v[c][j];
+                if (FIT == WHOLE || at + j < n) q += v[c][j] * v[c][j];
             }
-            sq[0] += CUT || at < n ? q : 0.f;
+            sq[0] += FIT != WHOLE || at < n ? q : 0.f;
         }
         team_join<BLOCK>(sq, lds[1]);
         const float rs = 1.0f / sqrtf(sq[0] / (float)n + eps);
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(BLOCK, BLOCK <= 512 ? 6 : 4) void layer_norm_forwar
         for (int c = 0; c < CHUNKS; ++c) {
 #pragma unroll
             for (int j = 0; j < V; ++j) v[c][j] = v[c][j] * rs * ga[c][j] + be[c][j];
-            store_chunk(y + r * ldy, (c * BLOCK + tid) * V, n, v[c]);
+            store_chunk<FIT>(y + r * ldy, (c * BLOCK + tid) * V, n, v[c]);
         }
         if (r2 >= rows) return;
         r = r2;
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T *
     Raw<T> kept[LONG_KEPT];
     float sum[1] = {0.f}, sq[1] = {0.f};
 #pragma unroll
-    for (int c = 0; c < LONG_KEPT; ++c) kept[c] = load_raw(row, first + c * STEP, n);
+    for (int c = 0; c < LONG_KEPT; ++c) kept[c] = load_raw<CUT>(row, first + c * STEP, n);
     // f(v, at) for every chunk of the thread that begins inside the row, zero outside it
     auto each = [&](auto f) {
         float v[V];
@@ -138,12 +138,12 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T *
                 f(v, first + c * STEP);
             }
         for (int at = first + LONG_KEPT * STEP; at < n; at += STEP) {
-            load_chunk(row, at, n, 0.f, v);
+            load_chunk(row, at, n, v);
             f(v, at);
         }
     };
 #pragma unroll
-    for (int c = 0; c < LONG_KEPT; ++c) settle<true>(kept[c], first + c * STEP, n);
+    for (int c = 0; c < LONG_KEPT; ++c) settle<CUT>(kept[c], first + c * STEP, n);
     each([&](float(&v)[V], int) {
 #pragma unroll
         for (int j = 0; j < V; ++j) sum[0] += v[j];
@@ -165,13 +165,13 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T *
     }
     each([&](float(&v)[V], int at) {
         float w[V];
-        load_columns<V>(gamma, at, n, 1.f, w);
+        load_columns<CUT, V>(gamma, at, n, 1.f, w);
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = (v[j] - mu) * rs * w[j];
-        load_columns<V>(beta, at, n, 0.f, w);
+        load_columns<CUT, V>(beta, at, n, 0.f, w);
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] += w[j];
-        store_chunk(y + r * ldy, at, n, v);
+        store_chunk<CUT>(y + r * ldy, at, n, v);
     });
 }
 
@@ -184,13 +184,13 @@ template <typename T> struct NormBackward {
     T *dx;
     int64_t lddx;
     float *dgamma, *dbeta, *part;  // part [ranges or workgroups][2][n], null: the sums go to dgamma and dbeta themselves
-    int tiles, narrow;             // tiles of columns, and whether they are of 4 chunks
+    int tiles, tile;               // tiles of columns, and their chunks
     int64_t range;                 // rows of a range
 };
 
 // The weights' gradients of one tile of columns, TILE chunks across, over one range of rows by a workgroup of 1024: 1024 / TILE
 // rows at a time, four of them a thread in flight.
-template <int TILE, typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, int tile, int64_t which, float *lds)
+template <int TILE, Fit FIT, typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, int tile, int64_t which, float *lds)
 {
     constexpr int V = CHUNK<T>, LANES = 1024 / TILE, ROWS = 4;
     const int col = threadIdx.x % TILE, lane = threadIdx.x / TILE, at = (tile * TILE + col) * V;
@@ -204,8 +204,8 @@ template <int TILE, typename T> __device__ __forceinline__ void norm_columns(con
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             const int64_t k = r + i * LANES < r1 ? r + i * LANES : r;
-            x[i] = load_raw(a.x + k * a.ldx, at, a.n);
-            d[i] = load_raw(a.dy + k * a.lddy, at, a.n);
+            x[i] = load_raw<FIT>(a.x + k * a.ldx, at, a.n);
+            d[i] = load_raw<FIT>(a.dy + k * a.lddy, at, a.n);
             mu[i] = a.mean[k];
             rs[i] = a.rstd[k];
         }
@@ -213,8 +213,8 @@ template <int TILE, typename T> __device__ __forceinline__ void norm_columns(con
         for (int i = 0; i < ROWS; ++i) {
             if (r + i * LANES >= r1) break;
             float xv[V], dv[V];
-            settle<true>(x[i], at, a.n);
-            settle<true>(d[i], at, a.n);
+            settle<FIT>(x[i], at, a.n);
+            settle<FIT>(d[i], at, a.n);
             unpack(x[i].w, xv);
             unpack(d[i].w, dv);
 #pragma unroll
@@ -243,31 +243,33 @@ template <int TILE, typename T> __device__ __forceinline__ void norm_columns(con
     }
 }
 
-// Tiles of 8 chunks, 128 bytes of a row and so a cache line, where there are enough of them to occupy the chip, else of 4.
+// Tiles of 8 chunks, 128 bytes of a row and so a cache line, where there are enough of them to occupy the chip, else of 4 (2048 x 4096
+// fp32: 27 us with tiles of 8, 38 of 4; 2000 x 2000 bf16: 15.8 and 13.2): a compute unit has only so many lines under way.
 constexpr int LN_TILE = 8, LN_NARROW = 4, LN_LDS = 16 * 2 * 8 * LN_TILE;
-template <typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, int id, float *lds)
+template <Fit FIT, typename T> __device__ __forceinline__ void norm_columns(const NormBackward<T> &a, int id, float *lds)
 {
     const int tile = id % a.tiles, which = id / a.tiles;
-    if (a.narrow) norm_columns<LN_NARROW>(a, tile, which, lds);
-    else norm_columns<LN_TILE>(a, tile, which, lds);
+    if (FIT == TINY || a.tile == LN_NARROW) norm_columns<LN_NARROW, FIT>(a, tile, which, lds);
+    else norm_columns<LN_TILE, FIT>(a, tile, which, lds);
 }
 
 // TEAM threads per row, 1024 / TEAM rows at a time, x and dy in registers between the sums and the output.  The first
-// tiles x ranges workgroups (`columns` of them) take the weights' gradients; the two kinds run beside each other, and what one
+// tiles x ranges workgroups (`columns` of them, counted over a grid's x and y: 2^28 columns are 2^23 tiles of fp32) take the weights' gradients; the two kinds run beside each other, and what one
 // reads the other finds in the caches.  With WEIGHTS there are none of that kind: a workgroup goes on to further rows, the next
 // row's loads in flight, adds their part of the weights' gradients in registers and leaves its sums in `part`.
-template <typename T, int TEAM, int CHUNKS, bool WEIGHTS, bool CUT>
-__global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(4, 4))) void layer_norm_backward_kernel(NormBackward<T> a, int columns)
+template <typename T, int TEAM, int CHUNKS, bool WEIGHTS, Fit FIT>
+__global__ __launch_bounds__(1024, 4) void layer_norm_backward_kernel(NormBackward<T> a, int columns)
 {
     constexpr int V = CHUNK<T>, TEAMS = 1024 / TEAM;
     __shared__ float lds[2][2][16];
     __shared__ float sums[WEIGHTS ? 1 : LN_LDS];
-    if (!WEIGHTS && (int)blockIdx.x < columns) {
-        norm_columns(a, blockIdx.x, sums);
+    const int64_t id = WEIGHTS ? blockIdx.x : grid_row() - columns, step = (int64_t)gridDim.x * TEAMS;
+    if (!WEIGHTS && id < 0) {
+        norm_columns<FIT>(a, (int)id + columns, sums);
         return;
     }
+    if (!WEIGHTS && (a.dx == nullptr || id * TEAMS >= a.rows)) return;
     const int team = threadIdx.x / TEAM, lane = threadIdx.x % TEAM;
-    const int64_t step = (int64_t)(gridDim.x - columns) * TEAMS;
     const float inv_n = 1.0f / (float)a.n;
     float ga[CHUNKS][V], dg[CHUNKS][V], db[CHUNKS][V];
     // rows in flight: two in fp32 (8192 x 4096: 95 us with one, 80 with two), whose chunks are half as many values (16384 x 4096 bf16:
@@ -275,39 +277,40 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(4, 4))) vo
     constexpr int AHEAD = WEIGHTS && V == 4 && CHUNKS == 1 ? 2 : 1;
     Raw<T> nx[AHEAD][CHUNKS], nd[AHEAD][CHUNKS];
     float nmu[AHEAD], nrs[AHEAD];
-    auto fetch = [&](int i, int64_t r) {  // (a row past the last one: zeros, which add nothing)
-        nmu[i] = r < a.rows ? a.mean[r] : 0.f;
-        nrs[i] = r < a.rows ? a.rstd[r] : 0.f;
+    auto fetch = [&](int i, int64_t r) {  // (of a row past the last one nothing is used)
+        if (r >= a.rows) return;
+        nmu[i] = a.mean[r];
+        nrs[i] = a.rstd[r];
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            const int n = r < a.rows ? a.n : 0;
-            nx[i][c] = load_raw(a.x + r * a.ldx, (c * TEAM + lane) * V, n);
-            nd[i][c] = load_raw(a.dy + r * a.lddy, (c * TEAM + lane) * V, n);
+            nx[i][c] = load_raw<FIT>(a.x + r * a.ldx, (c * TEAM + lane) * V, a.n);
+            nd[i][c] = load_raw<FIT>(a.dy + r * a.lddy, (c * TEAM + lane) * V, a.n);
         }
     };
-    int64_t r = (int64_t)(blockIdx.x - columns) * TEAMS + team;
+    int64_t r = id * TEAMS + team;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) fetch(i, r + i * step);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        load_columns<V>(a.gamma, (c * TEAM + lane) * V, a.n, 1.f, ga[c]);
+        if (WEIGHTS) load_columns<FIT, V>(a.gamma, (c * TEAM + lane) * V, a.n, 1.f, ga[c]);
 #pragma unroll
         for (int j = 0; j < V; ++j) dg[c][j] = db[c][j] = 0.f;
     }
     for (int turn = 0;; turn ^= 1, r += step) {
         float xh[CHUNKS][V], d[CHUNKS][V], s[2] = {0.f, 0.f};
         const float mu = nmu[0], rs = nrs[0];
+        const int n = r < a.rows ? a.n : 0;  // a row past the last one is zeros, which add nothing
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            settle<CUT>(nx[0][c], (c * TEAM + lane) * V, a.n);
-            settle<CUT>(nd[0][c], (c * TEAM + lane) * V, a.n);
+            settle<FIT>(nx[0][c], (c * TEAM + lane) * V, n);
+            settle<FIT>(nd[0][c], (c * TEAM + lane) * V, n);
             unpack(nx[0][c].w, xh[c]);
             unpack(nd[0][c].w, d[c]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) xh[c][j] = (c * TEAM + lane) * V + j < a.n ? (xh[c][j] - mu) * rs : 0.f;
+            for (int j = 0; j < V; ++j) xh[c][j] = (c * TEAM + lane) * V + j < n ? (xh[c][j] - mu) * rs : 0.f;
         }
-        const bool more = r - team + step < a.rows;  // (the same for the whole workgroup)
-        if (WEIGHTS && more) {
+        const bool more = WEIGHTS && r - team + step < a.rows;  // (the same for the whole workgroup)
+        if (more) {
 #pragma unroll
             for (int i = 0; i + 1 < AHEAD; ++i) {
                 nmu[i] = nmu[i + 1], nrs[i] = nrs[i + 1];
@@ -315,9 +318,11 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(4, 4))) vo
                 for (int c = 0; c < CHUNKS; ++c) nx[i][c] = nx[i + 1][c], nd[i][c] = nd[i + 1][c];
             }
             fetch(AHEAD - 1, r + AHEAD * step);
+            __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c)
+        for (int c = 0; c < CHUNKS; ++c) {
+            if (!WEIGHTS) load_columns<FIT, V>(a.gamma, (c * TEAM + lane) * V, a.n, 1.f, ga[c]);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 if (WEIGHTS) {
@@ -328,6 +333,7 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(4, 4))) vo
                 s[0] += d[c][j];
                 s[1] += d[c][j] * xh[c][j];
             }
+        }
         team_join<TEAM>(s, lds[turn]);
         const float mg = s[0] * inv_n, mgx = s[1] * inv_n;
         if (a.dx != nullptr && r < a.rows)
@@ -335,13 +341,13 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(4, 4))) vo
             for (int c = 0; c < CHUNKS; ++c) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) d[c][j] = rs * (d[c][j] - mg - xh[c][j] * mgx);
-                store_chunk(a.dx + r * a.lddx, (c * TEAM + lane) * V, a.n, d[c]);
+                store_chunk<FIT>(a.dx + r * a.lddx, (c * TEAM + lane) * V, a.n, d[c]);
             }
         if (!more) break;
     }
     if (!WEIGHTS || a.part == nullptr) return;
     // the teams' sums, a team after the other
-    float *part = a.part + (int64_t)blockIdx.x * 2 * a.n;
+    float *part = a.part + id * 2 * a.n;
     extern __shared__ float rows_lds[];  // [2][CHUNKS][V][TEAM]
     for (int t = TEAMS - 1; t > 0; --t) {
         __syncthreads();
@@ -372,15 +378,15 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(4, 4))) vo
 }
 
 // Rows of more chunks than that: the first LONG_KEPT chunks a thread of x and dy are kept as they lie in memory, what is beyond
-// them is read a second time from the caches.  (2^28 columns are 2^22 tiles of bf16, 2^23 of fp32: more than a grid's x takes.)
+// them is read a second time from the caches.
 template <typename T> __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(NormBackward<T> a, int columns)
 {
     constexpr int V = CHUNK<T>, STEP = 1024 * V, KEPT = LONG_KEPT / 2;
     __shared__ float lds[2][16];
     __shared__ float sums[LN_LDS];
-    const int64_t id = grid_row(), r = id - columns;
-    if (id < columns) {
-        norm_columns(a, (int)id, sums);
+    const int64_t r = grid_row() - columns;
+    if (r < 0) {
+        norm_columns<CUT>(a, (int)r + columns, sums);
         return;
     }
     if (a.dx == nullptr || r >= a.rows) return;
@@ -391,14 +397,14 @@ template <typename T> __global__ __launch_bounds__(1024) void layer_norm_backwar
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < KEPT; ++c) {
-        kx[c] = load_raw(xr, first + c * STEP, a.n);
-        kd[c] = load_raw(dr, first + c * STEP, a.n);
+        kx[c] = load_raw<CUT>(xr, first + c * STEP, a.n);
+        kd[c] = load_raw<CUT>(dr, first + c * STEP, a.n);
     }
     // f(xh, g, at) for every chunk of the thread; g is zero outside the row
     auto each = [&](auto f) {
         float x[V], d[V], g[V];
         auto give = [&](int at) {
-            load_columns<V>(a.gamma, at, a.n, 1.f, g);
+            load_columns<CUT, V>(a.gamma, at, a.n, 1.f, g);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 x[j] = at + j < a.n ? (x[j] - mu) * rs : 0.f;
@@ -414,15 +420,15 @@ template <typename T> __global__ __launch_bounds__(1024) void layer_norm_backwar
                 give(first + c * STEP);
             }
         for (int at = first + KEPT * STEP; at < a.n; at += STEP) {
-            load_chunk(xr, at, a.n, 0.f, x);
-            load_chunk(dr, at, a.n, 0.f, d);
+            load_chunk(xr, at, a.n, x);
+            load_chunk(dr, at, a.n, d);
             give(at);
         }
     };
 #pragma unroll
     for (int c = 0; c < KEPT; ++c) {
-        settle<true>(kx[c], first + c * STEP, a.n);
-        settle<true>(kd[c], first + c * STEP, a.n);
+        settle<CUT>(kx[c], first + c * STEP, a.n);
+        settle<CUT>(kd[c], first + c * STEP, a.n);
     }
     each([&](float(&x)[V], float(&d)[V], int) {
 #pragma unroll
@@ -436,7 +442,7 @@ template <typename T> __global__ __launch_bounds__(1024) void layer_norm_backwar
     each([&](float(&x)[V], float(&d)[V], int at) {
 #pragma unroll
         for (int j = 0; j < V; ++j) d[j] = rs * (d[j] - mg - x[j] * mgx);
-        store_chunk(a.dx + r * a.lddx, at, a.n, d);
+        store_chunk<CUT>(a.dx + r * a.lddx, at, a.n, d);
     });
 }
 
@@ -464,14 +470,17 @@ __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const float *__re
 // ------------------------------------------------------------------------------------------------ host side
 // How the weights' gradients are added.  fused: by the workgroups that take the rows, whose sums (8 bytes a column and workgroup,
 // written and read once) are then less than x and dy read again; else beside them, by tiles of columns over ranges of rows.
-struct WeightsPlan { bool fused, narrow; int64_t parts, tiles; };
+// Rows of at most 8192 elements, 8 values a thread: with 16 the registers do not hold a row and both sums (4096 x 16384 bf16: 201 us
+// fused, 133 beside; 4096 x 8192 fp32: 85 and 126).  More than 2048 of them (2048 x 4096 bf16: 19.5 and 19.7; 1024 x 4096: 17 and 11).
+constexpr int64_t FUSED_MOST = 8192;
+struct WeightsPlan { bool fused; int tile; int64_t parts, tiles; };
 
 static WeightsPlan weights_plan(int dtype, int64_t rows, int64_t n)
 {
     const int64_t v = 16 / (int64_t)elem_size(dtype), chunks = (n + v - 1) / v;
-    WeightsPlan p = {false, chunks < 128 * LN_TILE, 1, 0};
-    p.tiles = p.narrow ? (chunks + LN_NARROW - 1) / LN_NARROW : (chunks + LN_TILE - 1) / LN_TILE;
-    if (rows > 2048 && chunks <= 2048) {
+    WeightsPlan p = {false, chunks >= 128 * LN_TILE ? LN_TILE : LN_NARROW, 1, 0};
+    p.tiles = (chunks + p.tile - 1) / p.tile;
+    if (rows > 2048 && n <= FUSED_MOST) {
         p.fused = true;
         p.parts = 256;  // one workgroup per compute unit
         return p;
@@ -495,11 +504,12 @@ static void launch_forward(const LayerNormArgs &a, float eps, const float *beta,
 {
     // workgroups that are resident at once: 24 wavefronts per compute unit
     const int64_t most = 256 * (24 / (BLOCK / 64)), groups = a.rows < most ? a.rows : most;
-#define OMNI_LN_FORWARD(CUT)                                                                                                                                              \
-    hipLaunchKernelGGL((layer_norm_forward_kernel<T, BLOCK, CHUNKS, CUT>), row_grid(groups), dim3(BLOCK), 0, s, (const T *)a.x, a.ldx, a.rows, (int)a.width, eps, a.gamma, beta, y, \
+#define OMNI_LN_FORWARD(FIT)                                                                                                                                              \
+    hipLaunchKernelGGL((layer_norm_forward_kernel<T, BLOCK, CHUNKS, FIT>), row_grid(groups), dim3(BLOCK), 0, s, (const T *)a.x, a.ldx, a.rows, (int)a.width, eps, a.gamma, beta, y, \
                        ldy, mean, rstd)
-    if (a.width % CHUNK<T> == 0) OMNI_LN_FORWARD(false);
-    else OMNI_LN_FORWARD(true);
+    if (a.width % CHUNK<T> == 0) OMNI_LN_FORWARD(WHOLE);
+    else if (BLOCK > 64 || CHUNKS > 1 || a.width > CHUNK<T>) OMNI_LN_FORWARD(CUT);
+    else OMNI_LN_FORWARD((BLOCK == 64 && CHUNKS == 1 ? TINY : CUT));
 #undef OMNI_LN_FORWARD
 }
 
@@ -529,9 +539,17 @@ template <typename T, int TEAM, int CHUNKS> static void launch_backward(const No
     constexpr int64_t TEAMS = 1024 / TEAM;
     const int64_t groups = (b.rows + TEAMS - 1) / TEAMS;
     const size_t lds = TEAMS > 1 ? 2 * CHUNKS * CHUNK<T> * TEAM * sizeof(float) : 0;
-    if (!fused) hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, false, true>), dim3((unsigned)(columns + (dx ? groups : 0))), dim3(1024), 0, s, b, (int)columns);
-    else if (b.n % CHUNK<T> == 0) hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, true, false>), dim3((unsigned)parts), dim3(1024), lds, s, b, 0);
-    else hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, true, true>), dim3((unsigned)parts), dim3(1024), lds, s, b, 0);
+    const Fit fit = b.n % CHUNK<T> == 0 ? WHOLE : TEAM == 64 && b.n < CHUNK<T> ? TINY : CUT;
+    constexpr bool FUSES = TEAM * CHUNKS * CHUNK<T> <= FUSED_MOST;
+#define OMNI_LN_BACKWARD(FIT)                                                                                                                                               \
+    do {                                                                                                                                                                    \
+        if (FUSES && fused) hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, FUSES, FIT>), dim3((unsigned)parts), dim3(1024), lds, s, b, 0);                 \
+        else hipLaunchKernelGGL((layer_norm_backward_kernel<T, TEAM, CHUNKS, false, FIT>), row_grid(columns + (dx ? groups : 0)), dim3(1024), 0, s, b, (int)columns);          \
+    } while (0)
+    if (fit == WHOLE) OMNI_LN_BACKWARD(WHOLE);
+    else if (fit == CUT) OMNI_LN_BACKWARD(CUT);
+    else OMNI_LN_BACKWARD((TEAM == 64 ? TINY : CUT));
+#undef OMNI_LN_BACKWARD
 }
 
 template <typename T> static int backward_launch(const NormBackward<T> &b, bool fused, int64_t columns, int64_t parts, bool dx, hipStream_t s)
@@ -555,7 +573,7 @@ static int backward(const LayerNormArgs &a, const T *dy, int64_t lddy, const flo
     const bool weights = dgamma != nullptr || dbeta != nullptr;
     WeightsPlan p = weights_plan(a.dtype, a.rows, a.width);
     const int64_t range = p.fused ? a.rows : (a.rows + p.parts - 1) / p.parts, columns = p.tiles * p.parts;
-    NormBackward<T> b = {(const T *)a.x, dy, a.ldx, lddy, a.rows, (int)a.width, a.gamma, mean, rstd, dx, lddx, dgamma, dbeta, p.parts > 1 ? part : nullptr, (int)p.tiles, p.narrow ? 1 : 0, range};
+    NormBackward<T> b = {(const T *)a.x, dy, a.ldx, lddy, a.rows, (int)a.width, a.gamma, mean, rstd, dx, lddx, dgamma, dbeta, p.parts > 1 ? part : nullptr, (int)p.tiles, p.tile, range};
     int st;
     if (!weights) {  // (the resident workgroups are the faster ones for many rows, also without sums to leave)
         b.part = nullptr;

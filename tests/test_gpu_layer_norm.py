@@ -44,7 +44,7 @@ def make(rows, width, dtype, seed=1, mean=0.5, sigma=1.5):
 
 
 SHAPES = [(1, 1, 0), (3, 2, 1), (2, 7, 0), (5, 8, 0), (4, 63, 5), (7, 64, 0), (3, 65, 0), (2, 513, 3), (6, 1001, 0), (3, 2048, 0), (2, 2049, 7),
-          (2, 4097, 0), (3, 8200, 8), (2, 16391, 0), (1, 40001, 0), (2, 70000, 1), (700, 33, 0), (2100, 20, 4), (4099, 130, 1), (65, 9216, 0)]
+          (2, 4097, 0), (3, 8200, 8), (2, 16391, 0), (1, 40001, 0), (2, 70000, 1), (700, 33, 0), (2100, 20, 4), (4099, 130, 1), (65, 9216, 0), (4100, 8200, 0)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
