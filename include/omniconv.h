@@ -343,7 +343,8 @@ int omni_dropout_backward(int32_t dtype, int64_t count, float p, uint64_t seed, 
  * The end of a network: layer norm, what is read off its logits, and the loss that trains it.  Matrices are [rows][ld] of
  * `dtype`, of which the first width (classes) elements of a row count, ld >= width; the rest of a row is neither read nor
  * written, and ld need not be a multiple of anything.  Everything else is dense: fp32 per row or per column, indexes int64.
- * Arithmetic in fp32, one rounding on store.  An output may be the input named with it below, with the same ld; no other
+ * Arithmetic in fp32, one rounding on store; the order of a sum is decided by the sizes and, for logits, by where a row begins
+ * within 16 bytes, so the same call gives the same bits.  An output may be the input named with it below, with the same ld; no other
  * buffers may overlap.  rows == 0 launches nothing (layer_norm_backward then clears dgamma and dbeta).  A workspace sized for
  * the most rows serves fewer.
  *

@@ -103,7 +103,7 @@ __global__ __launch_bounds__(BLOCK, BLOCK <= 512 ? (FIT == CUT && BLOCK == 512 ?
         for (int c = 0; c < CHUNKS; ++c) {
 #pragma unroll
             for (int j = 0; j < V; ++j) v[c][j] = v[c][j] * rs * ga[c][j] + be[c][j];
-            store_chunk<FIT>(y + r * ldy, (c * BLOCK + tid) * V, n, v[c]);
+            store_chunk<FIT>(y + r * ldy, (c * BLOCK + tid) * V, n, v[c], false);
         }
         if (r2 >= rows) return;
         r = r2;
@@ -171,11 +171,13 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T *
         load_columns<CUT, V>(beta, at, n, 0.f, w);
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] += w[j];
-        store_chunk<CUT>(y + r * ldy, at, n, v);
+        store_chunk<CUT>(y + r * ldy, at, n, v, false);
     });
 }
 
 // ------------------------------------------------------------------------------------------------ backward
+__device__ __forceinline__ bool on16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
 template <typename T> struct NormBackward {
     const T *x, *dy;
     int64_t ldx, lddy, rows;
@@ -186,6 +188,7 @@ template <typename T> struct NormBackward {
     float *dgamma, *dbeta, *part;  // part [ranges or workgroups][2][n], null: the sums go to dgamma and dbeta themselves
     int tiles, tile;               // tiles of columns, and their chunks
     int64_t range;                 // rows of a range
+    bool past;                     // dx goes past the caches
 };
 
 // The weights' gradients of one tile of columns, TILE chunks across, over one range of rows by a workgroup of 1024: 1024 / TILE
@@ -341,7 +344,7 @@ __global__ __launch_bounds__(1024, 4) void layer_norm_backward_kernel(NormBackwa
             for (int c = 0; c < CHUNKS; ++c) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) d[c][j] = rs * (d[c][j] - mg - xh[c][j] * mgx);
-                store_chunk<FIT>(a.dx + r * a.lddx, (c * TEAM + lane) * V, a.n, d[c]);
+                store_chunk<FIT>(a.dx + r * a.lddx, (c * TEAM + lane) * V, a.n, d[c], a.past && on16(a.dx + r * a.lddx));
             }
         if (!more) break;
     }
@@ -442,7 +445,7 @@ template <typename T> __global__ __launch_bounds__(1024) void layer_norm_backwar
     each([&](float(&x)[V], float(&d)[V], int at) {
 #pragma unroll
         for (int j = 0; j < V; ++j) d[j] = rs * (d[j] - mg - x[j] * mgx);
-        store_chunk<CUT>(a.dx + r * a.lddx, at, a.n, d);
+        store_chunk<CUT>(a.dx + r * a.lddx, at, a.n, d, a.past && on16(a.dx + r * a.lddx));
     });
 }
 
@@ -573,7 +576,7 @@ static int backward(const LayerNormArgs &a, const T *dy, int64_t lddy, const flo
     const bool weights = dgamma != nullptr || dbeta != nullptr;
     WeightsPlan p = weights_plan(a.dtype, a.rows, a.width);
     const int64_t range = p.fused ? a.rows : (a.rows + p.parts - 1) / p.parts, columns = p.tiles * p.parts;
-    NormBackward<T> b = {(const T *)a.x, dy, a.ldx, lddy, a.rows, (int)a.width, a.gamma, mean, rstd, dx, lddx, dgamma, dbeta, p.parts > 1 ? part : nullptr, (int)p.tiles, p.tile, range};
+    NormBackward<T> b = {(const T *)a.x, dy, a.ldx, lddy, a.rows, (int)a.width, a.gamma, mean, rstd, dx, lddx, dgamma, dbeta, p.parts > 1 ? part : nullptr, (int)p.tiles, p.tile, range, past_caches(a.dtype, a.rows, a.width)};
     int st;
     if (!weights) {  // (the resident workgroups are the faster ones for many rows, also without sums to leave)
         b.part = nullptr;

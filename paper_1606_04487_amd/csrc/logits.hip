@@ -547,7 +547,7 @@ template <int MOST> struct ListLds {
 // Chunks [c0, c1) of a row, aligned as the output's row is, AHEAD of them loaded before the first is used; `also` may change a
 // chunk's values before they are rounded.
 template <Fit FIT, typename T, int BLOCK, int AHEAD, typename F, typename G>
-__device__ __forceinline__ void write_chunks(const T *in, T *out, int n, int shift, int64_t c0, int64_t c1, F value, G also)
+__device__ __forceinline__ void write_chunks(const T *in, T *out, int n, int shift, int64_t c0, int64_t c1, bool past, F value, G also)
 {
     constexpr int V = CHUNK<T>;
     for (int64_t c = c0 + threadIdx.x; c < c1; c += AHEAD * BLOCK) {
@@ -564,17 +564,17 @@ __device__ __forceinline__ void write_chunks(const T *in, T *out, int n, int shi
 #pragma unroll
             for (int j = 0; j < V; ++j) x[j] = value(x[j]);
             also(at, x);
-            store_chunk<FIT>(out, at, n, x);
+            store_chunk<FIT>(out, at, n, x, past);
         }
     }
 }
-template <typename T, int BLOCK, int AHEAD, typename F, typename G> __device__ __forceinline__ void write_row(const T *in, T *out, int n, int64_t c0, int64_t c1, F value, G also)
+template <typename T, int BLOCK, int AHEAD, typename F, typename G> __device__ __forceinline__ void write_row(const T *in, T *out, int n, int64_t c0, int64_t c1, bool past, F value, G also)
 {
     constexpr int V = CHUNK<T>;
     const int shift = (int)(((uintptr_t)out / sizeof(T)) % V);
     if (c1 > (n + shift + V - 1) / V) c1 = (n + shift + V - 1) / V;
-    if (n >= V) write_chunks<CUT, T, BLOCK, AHEAD>(in, out, n, shift, c0, c1, value, also);
-    else write_chunks<TINY, T, BLOCK, 1>(in, out, n, shift, c0, c1, value, also);
+    if (n >= V) write_chunks<CUT, T, BLOCK, AHEAD>(in, out, n, shift, c0, c1, past, value, also);
+    else write_chunks<TINY, T, BLOCK, 1>(in, out, n, shift, c0, c1, past, value, also);
 }
 
 // The listed classes in the elements that a call of write_row with the same chunks covers: their logits (before), their values
@@ -625,13 +625,14 @@ template <typename T, int BLOCK, int MOST> struct ListedOut {
 // A workgroup writes 4 chunks a thread of a row (distillation's gradient of 4096 x 65536 bf16: 184 us, 262 with 16 chunks a
 // thread).  One wavefront where that is the row, which then needs no barriers (log probabilities' of 16384 x 1000 bf16: 57 us with
 // workgroups of 256, 14 so).
-struct Pieces { int block, count, chunks; };  // chunks of a piece
+struct Pieces { int block, count, chunks; bool past; };  // chunks of a piece; whether it is stored past the caches
 
-static Pieces grad_pieces(int64_t classes, int64_t v)
+static Pieces grad_pieces(int dtype, int64_t rows, int64_t classes)
 {
+    const int64_t v = 16 / (int64_t)elem_size(dtype);
     const int64_t chunks = (classes + v - 1) / v + 1;  // one more than the row has: they are counted from an aligned address in front of it
     const int block = chunks <= 4 * 64 ? 64 : 256;
-    return {block, (int)((chunks + 4 * block - 1) / (4 * block)), 4 * block};
+    return {block, (int)((chunks + 4 * block - 1) / (4 * block)), 4 * block, past_caches(dtype, rows, classes)};
 }
 
 // ONE: at most one target a row, which is added where its chunk is written; else the targets are a list.
@@ -676,7 +677,7 @@ __global__ __launch_bounds__(BLOCK) void logprob_backward_kernel(const T *logits
     };
     if (ONE) {
         const int at0 = target >= 0 && target < n ? (int)target : -V;
-        write_row<T, BLOCK, 4>(in, to, n, c0, c1, value, [&](int at, float(&x)[V]) {
+        write_row<T, BLOCK, 4>(in, to, n, c0, c1, pieces.past, value, [&](int at, float(&x)[V]) {
             if ((unsigned)(at0 - at) < (unsigned)V)
 #pragma unroll
                 for (int j = 0; j < V; ++j) x[j] += at + j == at0 ? all : 0.f;
@@ -686,7 +687,7 @@ __global__ __launch_bounds__(BLOCK) void logprob_backward_kernel(const T *logits
     ListedOut<T, BLOCK, ONE ? 1 : GIVEN_MOST> listed;
     listed.read(in, to, n, c0, c1, l, given);
     __syncthreads();
-    write_row<T, BLOCK, 4>(in, to, n, c0, c1, value, [](int, float(&)[V]) {});
+    write_row<T, BLOCK, 4>(in, to, n, c0, c1, pieces.past, value, [](int, float(&)[V]) {});
     __syncthreads();
     listed.write(to, l, given, value);
 }
@@ -694,7 +695,7 @@ __global__ __launch_bounds__(BLOCK) void logprob_backward_kernel(const T *logits
 template <typename T> static int logprob_backward(const LogitsArgs &a, const int64_t *targets, int given, const float *dlogprob, const float *dentropy, const float *entropy,
                                                   const float *stats, T *out, int64_t ld_out, hipStream_t s)
 {
-    const Pieces pieces = grad_pieces(a.classes, CHUNK<T>);
+    const Pieces pieces = grad_pieces(a.dtype, a.rows, a.classes);
 #define OMNI_LOGPROB_BACKWARD(B, ONE)                                                                                                                                           \
     hipLaunchKernelGGL((logprob_backward_kernel<T, B, ONE>), row_grid(a.rows * pieces.count), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, LOG2E / a.temperature, \
                        1.f / a.temperature, targets, given, dlogprob, dentropy, entropy, stats, out, ld_out)
@@ -936,7 +937,7 @@ __global__ __launch_bounds__(JOIN_BLOCK) void distill_join_kernel(const T *__res
 // a longer row has beyond them is read again.
 template <typename T, int BLOCK, int KEPT, int ALSO>
 __global__ __launch_bounds__(BLOCK) void distill_both_kernel(const T *logits, int64_t ld, int64_t rows, int n, DistillArgs d, float c, float *__restrict__ loss, T *out,
-                                                             int64_t ld_out)
+                                                             int64_t ld_out, int past)
 {
     constexpr int V = CHUNK<T>;
     __shared__ float lds[2 * (BLOCK / 64)];
@@ -955,14 +956,13 @@ __global__ __launch_bounds__(BLOCK) void distill_both_kernel(const T *logits, in
     listed.read(row, n, l, k.count);
     const float edge = (int)threadIdx.x < sp.edges ? element(row + sp.edge(threadIdx.x, n)) : 0.f;
     __syncthreads();
+    const bool aligned = past && ((uintptr_t)to / sizeof(T)) % V == sp.shift;
     auto put = [&](const uint4 &b, int c) {
         float x[V];
         unpack<T>(b, x);
 #pragma unroll
         for (int j = 0; j < V; ++j) x[j] = value(x[j]);
-        ChunkBits<T> w;
-        pack(x, w.w);
-        *reinterpret_cast<ChunkBits<T> *>(to + sp.first(c)) = w;
+        store_whole(to + sp.first(c), x, aligned);
     };
     int at = sp.lo + threadIdx.x;
 #pragma unroll
@@ -1004,7 +1004,7 @@ __global__ __launch_bounds__(BLOCK) void distill_backward_kernel(const T *logits
     listed.read(in, to, n, c0, c1, l, k.count);
     __syncthreads();
     // (1021 x 32003 fp32: 47 us with one chunk ahead, 50 with four; 4096 x 65536 bf16: 197 and 184)
-    write_row<T, BLOCK, sizeof(T) == 4 ? 1 : 4>(in, to, n, c0, c1, value, [](int, float(&)[CHUNK<T>]) {});
+    write_row<T, BLOCK, sizeof(T) == 4 ? 1 : 4>(in, to, n, c0, c1, pieces.past, value, [](int, float(&)[CHUNK<T>]) {});
     __syncthreads();
     listed.write(to, l, k.count, value);
 }
@@ -1065,7 +1065,7 @@ template <typename T>
 static int distill_backward(const LogitsArgs &a, const DistillArgs &d, const float *stats, const float4 *sums, int parts, float *loss, T *out, int64_t ld_out, hipStream_t s)
 {
     const float c = distill_scale(d);
-    const Pieces pieces = grad_pieces(a.classes, CHUNK<T>);
+    const Pieces pieces = grad_pieces(a.dtype, a.rows, a.classes);
 #define OMNI_DISTILL_BACKWARD(B, ALSO)                                                                                                                              \
     hipLaunchKernelGGL((distill_backward_kernel<T, B, ALSO>), row_grid(a.rows * pieces.count), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, pieces, d, c, stats, \
                        sums, parts, loss, out, ld_out)
@@ -1097,8 +1097,9 @@ template <typename T> static int distill_both(const LogitsArgs &a, const Distill
         OMNI_LAUNCH_CHECK();
         return distill_backward<T>(a, d, nullptr, sums, p.count, over ? nullptr : loss, out, ld_out, s);
     }
+    const int past = past_caches(a.dtype, a.rows, a.classes);
 #define OMNI_DISTILL_BOTH(B, K, ALSO) \
-    hipLaunchKernelGGL((distill_both_kernel<T, B, K, ALSO>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, d, c, loss, out, ld_out)
+    hipLaunchKernelGGL((distill_both_kernel<T, B, K, ALSO>), row_grid(a.rows), dim3(B), 0, s, (const T *)a.logits, a.ld, a.rows, (int)a.classes, d, c, loss, out, ld_out, past)
     if (chunks <= 256) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 64, 4);
     else if (chunks <= 1024) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 256, 4);
     else if (chunks <= 2048) OMNI_BY_SECOND(OMNI_DISTILL_BOTH, 256, 8);

@@ -244,3 +244,16 @@ def test_rows_of_three_dimensions_and_what_is_refused(B):
     rows = torch.zeros(4099, device="cuda")
     with pytest.raises((ValueError, B.OmniError)):
         B.layer_norm_backward(many, many, rows, rows, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype,rows,width", [(torch.bfloat16, 17000, 4096), (torch.float32, 8400, 4099), (torch.bfloat16, 4100, 16400)])
+def test_large_gradients_are_those_of_their_rows(B, dtype, rows, width):
+    # more than 2^27 bytes of dx, rows that begin anywhere
+    x, dy = torch.randn(rows, width, device="cuda").to(dtype), torch.randn(rows, width, device="cuda").to(dtype)
+    gamma = torch.randn(width, device="cuda")
+    _, mean, rstd = B.layer_norm_forward(x, gamma)
+    dx, _, _ = B.layer_norm_backward(x, dy, mean, rstd, gamma)
+    half = rows // 4 * 2
+    for s in (slice(0, half), slice(half, rows)):
+        part, _, _ = B.layer_norm_backward(x[s].clone(), dy[s].clone(), mean[s].clone(), rstd[s].clone(), gamma)
+        assert torch.equal(part, dx[s])

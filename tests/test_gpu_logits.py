@@ -462,3 +462,30 @@ def test_widest_row(B):
     assert np.all(np.abs(got - (p - np.array([q[0], q[1], 0.0, 0.0]))) <= tol * np.array([1.0, 1.0, p[2], p[3]]))
     del x, grad, both
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("extra", [0, 7])
+def test_large_gradients_are_those_of_their_rows(B, extra):
+    # more than 2^27 bytes of results, rows that begin anywhere, and outputs whose rows are aligned otherwise
+    rows, n, k = 2100, 33001, 4
+    x = logits(rows, n, torch.bfloat16)
+    index, labels = torch.randint(0, n, (rows, k)).cuda(), torch.randint(0, n, (rows,)).cuda()
+    best, w, stats = torch.randn(rows, k).cuda(), torch.rand(rows).cuda(), None
+    out = [pitched(torch.zeros_like(x), extra, 3.0) for _ in range(3)]
+    loss, _ = B.distill_forward_backward(x, index, best, labels, 2.0, 0.5, dloss=w, dlogits=out[0])
+    _, stats = B.distill_forward(x, index, best, labels, 2.0, 0.5)
+    B.distill_backward(x, index, best, labels, 2.0, 0.5, stats=stats, dloss=w, dlogits=out[1])
+    lp, h, _, _, st = B.logprob_forward(x, labels)
+    B.logprob_backward(x, st, labels, w, w, h, dlogits=out[2])
+    # A row's sums are taken in an order that depends on where it begins within 16 bytes, so the parts begin at whole multiples of 8
+    # rows: there a row of the part begins where it does in the whole.
+    for a in range(0, rows, 704):
+        s = slice(a, a + 704)
+        part = x[s].clone()
+        l, d = B.distill_forward_backward(part, index[s].clone(), best[s].clone(), labels[s].clone(), 2.0, 0.5, dloss=w[s].clone())
+        assert torch.equal(l, loss[s]) and torch.equal(d, out[0][s])
+        d = B.distill_backward(part, index[s].clone(), best[s].clone(), labels[s].clone(), 2.0, 0.5, stats=stats[s].clone(), dloss=w[s].clone())
+        assert torch.equal(d, out[1][s])
+        d = B.logprob_backward(part, st[s].clone(), labels[s].clone(), w[s].clone(), w[s].clone(), h[s].clone())
+        assert torch.equal(d, out[2][s])
+    assert all(untouched(t, extra, 3.0) for t in out)
