@@ -239,7 +239,7 @@ constexpr int TOP_KEYS = 512, TOP_LIST = 256;
 template <int BLOCK> struct TopLds {
     uint64_t keys[TOP_KEYS];
     uint64_t bar;
-    uint32_t group[BLOCK];
+    alignas(16) uint32_t group[BLOCK];
     int count, listed;
     uint16_t list[TOP_LIST];  // slot * BLOCK + thread
 };
@@ -253,41 +253,65 @@ template <int BLOCK> struct TopLds {
 // (equal values), the k-th largest of those collected is a higher bound, and the collection is done again: every key is
 // different, so this ends.
 template <typename T, int BLOCK, int KEPT, typename PUT>
-__device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &sp, float own, int k, TopLds<BLOCK> &t, const uint4 (&kept)[KEPT > 0 ? KEPT : 1],
+__device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &sp, float own, int k, TopLds<BLOCK> &t, uint4 (&kept)[KEPT > 0 ? KEPT : 1],
                                         const Slots<BLOCK> *slots, int shift, PUT put)
 {
     static_assert(BLOCK == 256 || (BLOCK == 64 && KEPT > 0), "groups of a lane");
-    constexpr int V = CHUNK<T>, EACH = BLOCK == 64 ? KEPT : 4;  // groups that a lane compares
+    constexpr int V = CHUNK<T>, EACH = BLOCK == 64 ? KEPT : 4;  // groups of a lane
     const int tid = threadIdx.x, lane = tid & 63, rest = KEPT > 0 ? sp.hi : sp.lo;
-    uint32_t u[EACH], bound = 0;
-    int groups = EACH;
-    if (BLOCK == 64 && k <= 16) {  // (then 64 groups, the lanes, bound as well)
-        groups = 1;
-        u[0] = ordered(own);
-    } else if constexpr (BLOCK == 64) {  // every chunk is a group
+    // The kept chunks are unpacked again where they are looked through, and their indexes taken again: held since the sums, or over the
+    // repetitions, they are 166 registers instead of 94 (5 of 4096 x 4096 bf16: 22 us, 13.5 so; of 16384 x 1000: 31 and 21).
+    auto as_they_lie = [&]() {
+        if (KEPT > 0)
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            float x[V], g = i == 0 && tid < sp.edges ? element(row + sp.edge(tid, n)) : -INFINITY;
-            unpack<T>(kept[i], x);
-#pragma unroll
-            for (int j = 0; j < V; ++j) g = sp.lo + tid + i * 64 < sp.hi ? fmaxf(g, x[j]) : g;
-            u[i] = ordered(fmaxf(g, -INFINITY));
+            for (int i = 0; i < KEPT; ++i) asm volatile("" : "+v"(kept[i].x), "+v"(kept[i].y), "+v"(kept[i].z), "+v"(kept[i].w));
+    };
+    uint32_t bound = 0;
+    if (tid == 0) t.listed = 0;
+    as_they_lie();
+    // 16 or fewer: 64 groups bound as well, and every lane counts the maxima above its own.  More: the bound by its bits, from the
+    // highest (counting over 256 groups: 32 of 2047 x 50021 bf16 53 us, by bits 47).
+    if (k <= 16) {
+        float g = own;
+        if (BLOCK == 256) {
+            g = fmaxf(g, dpp<0xb1>(g));
+            g = fmaxf(g, dpp<0x4e>(g));
         }
-    } else {  // every thread is
-        t.group[tid] = ordered(own);
-        if (tid == 0) t.listed = 0;
+        if (tid % (BLOCK / 64) == 0) t.group[tid / (BLOCK / 64)] = ordered(g);
         __syncthreads();
+        const uint32_t mine = t.group[lane];
+        int above = 0;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) u[i] = t.group[i * 64 + lane];
-    }
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t more = bound | (1u << bit);
-        int reach = 0;
+        for (int i = 0; i < 64; i += 4) {
+            const uint4 o = *reinterpret_cast<const uint4 *>(t.group + i);
+            above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+        }
+        bound = __float_as_uint(wave_join(__uint_as_float(above < k ? mine : ~0u), MinBits()));
+    } else {
+        uint32_t u[EACH];
+        if constexpr (BLOCK == 64) {  // every chunk is a group
 #pragma unroll
-        for (int i = 0; i < EACH; ++i)
-            if (i < groups) reach += __popcll(__ballot(u[i] >= more));
-        if (reach >= k) bound = more;
-        if (reach == k) break;
+            for (int i = 0; i < EACH; ++i) {
+                float x[V], g = i == 0 && tid < sp.edges ? element(row + sp.edge(tid, n)) : -INFINITY;
+                unpack<T>(kept[i], x);
+#pragma unroll
+                for (int j = 0; j < V; ++j) g = sp.lo + tid + i * 64 < sp.hi ? fmaxf(g, x[j]) : g;
+                u[i] = ordered(fmaxf(g, -INFINITY));
+            }
+        } else {  // every thread is
+            t.group[tid] = ordered(own);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) u[i] = t.group[i * 64 + lane];
+        }
+        for (int bit = 31; bit >= (V == 8 ? 16 : 0); --bit) {  // (the lower half of a bf16 value's key says nothing)
+            const uint32_t more = bound | (1u << bit);
+            int reach = 0;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) reach += __popcll(__ballot(u[i] >= more));
+            if (reach >= k) bound = more;
+            if (reach == k) break;
+        }
     }
     if (bound <= ORDERED_NOTHING) bound = ORDERED_NOTHING + 1;  // -inf is nobody's alternative
     const bool able = ordered(own) >= bound;
@@ -305,12 +329,16 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
         __syncthreads();
         if (tid == 0) t.count = 0;
         __syncthreads();
+        as_they_lie();
+        int at = sp.lo + tid;
+        asm volatile("" : "+v"(at));
+        const float least = unordered((uint32_t)(bar >> 32));
         auto offer = [&](float x, int i) {
+            if (!(x >= least)) return;
             const uint64_t key = ((uint64_t)ordered(x) << 32) | (uint32_t)~i;
-            if (key >= bar && x > -INFINITY) {  // (NaN is not)
-                const int to = atomicAdd(&t.count, 1);
-                if (to < TOP_KEYS) t.keys[to] = key;
-            }
+            if (key < bar) return;
+            const int to = atomicAdd(&t.count, 1);
+            if (to < TOP_KEYS) t.keys[to] = key;
         };
         auto offer_chunk = [&](const uint4 &b, int c) {
             float x[V];
@@ -318,14 +346,14 @@ __device__ __forceinline__ void row_top(const T *row, int n, const RowSplit<T> &
             float most = x[0];
 #pragma unroll
             for (int j = 1; j < V; ++j) most = fmaxf(most, x[j]);
-            if (ordered(most) < (uint32_t)(bar >> 32)) return;
+            if (!(most >= least)) return;
 #pragma unroll
             for (int j = 0; j < V; ++j) offer(x[j], sp.first(c) + j);
         };
         if (able) {
 #pragma unroll
             for (int i = 0; i < KEPT; ++i)
-                if (sp.lo + tid + i * BLOCK < sp.hi) offer_chunk(kept[i], sp.lo + tid + i * BLOCK);
+                if (at + i * BLOCK < sp.hi) offer_chunk(kept[i], at + i * BLOCK);
             if (tid < sp.edges) offer(element(row + sp.edge(tid, n)), sp.edge(tid, n));
         }
         const int listed = KEPT > 0 ? 0 : t.listed;
@@ -441,28 +469,29 @@ template <int ALSO> __device__ __forceinline__ Sums join_parts(const float4 *sum
 }
 
 // The k largest of the parts' k largest by a workgroup of 256, as in row_top: the k-th largest of the threads' maxima is the bound,
-// here of whole keys, so that few more than k reach it whatever is equal.  found [parts * k].
+// here of whole keys, so that few more than k reach it whatever is equal; by counting (20 of 48 x 131072 bf16: 15.4 us, 17.4 by bits).
+// found [parts * k].
 template <typename PUT> __device__ __forceinline__ void join_tops(const uint64_t *keys, int total, int k, uint64_t *found, PUT put)
 {
-    __shared__ uint64_t group[256];
+    __shared__ alignas(16) uint64_t group[256];
+    __shared__ uint64_t kth;
     __shared__ int count;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x;
     uint64_t own = 0;
     for (int i = tid; i < total; i += 256) own = keys[i] > own ? keys[i] : own;
     group[tid] = own;
-    if (tid == 0) count = 0;
+    if (tid == 0) count = 0, kth = 0;
     __syncthreads();
-    uint64_t g[4], bound = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) g[i] = group[i * 64 + lane];
-    for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t more = bound | (1ull << bit);
-        int reach = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) reach += __popcll(__ballot(g[i] >= more));
-        if (reach >= k) bound = more;
-        if (reach == k) break;
+    // (every key but 0 is different: the one with k - 1 above it is the k-th)
+    int over = 0;
+#pragma unroll 16
+    for (int i = 0; i < 256; i += 2) {
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(group + i);
+        over += (o.x > own) + (o.y > own);
     }
+    if (over == k - 1) kth = own;
+    __syncthreads();
+    uint64_t bound = kth;
     if (bound == 0) bound = 1;  // (a key of 0 is none)
     if (own >= bound)
         for (int i = tid; i < total; i += 256)

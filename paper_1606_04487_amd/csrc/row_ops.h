@@ -166,6 +166,7 @@ template <int STRIDE, typename OP> __device__ __forceinline__ float join_strided
     return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct MinBits { __device__ __forceinline__ float operator()(float a, float b) const { return __uint_as_float(min(__float_as_uint(a), __float_as_uint(b))); } };  // of whole numbers
 struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 
 // The workgroup's sum (or maximum) of N values a thread, to every thread.  `lds` holds N * BLOCK / 64 floats; the barrier in
