@@ -567,10 +567,15 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const T *__restrict__
 // ------------------------------------------------------------------------------------------------ gradients
 // A row's gradient is a function of the element and the row's sums everywhere but at a few listed classes, where something is
 // added.  `value` gives the first; the listed classes are written last, each with all that is added to it in one rounding, by
-// the first entry of the list that names it.  out may be the logits themselves.
+// the first entry of the list that names it: every entry looks through the list, four at a time (16384 x 1000 bf16 with 32 entries:
+// 23.5 us one at a time, 19.9 so; 1 x 1000 fp32, loss and gradient: 6.5 and 5.1).  out may be the logits themselves.
 template <int MOST> struct ListLds {
-    int64_t at[MOST];
-    float add[MOST];
+    alignas(16) int at[(MOST + 3) / 4 * 4];  // -1: not in the row
+    alignas(16) float add[(MOST + 3) / 4 * 4];
+    __device__ __forceinline__ void close(int count)  // fills the last four up; a barrier comes before the list is read by fours
+    {
+        if ((int)threadIdx.x < (-count & 3)) at[count + threadIdx.x] = -1;
+    }
 };
 
 // Chunks [c0, c1) of a row, aligned as the output's row is, AHEAD of them loaded before the first is used; `also` may change a
@@ -630,7 +635,7 @@ template <typename T, int BLOCK, int MOST> struct ListedOut {
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
             const int i = threadIdx.x + e * BLOCK;
-            if (i < count && l.at[i] >= 0 && l.at[i] < n) x[e] = element(in + l.at[i]);
+            if (i < count && l.at[i] >= 0) x[e] = element(in + l.at[i]);
         }
     }
     template <typename F> __device__ __forceinline__ void write(T *out, const ListLds<MOST> &l, int count, F value)
@@ -639,13 +644,18 @@ template <typename T, int BLOCK, int MOST> struct ListedOut {
         for (int e = 0; e < EACH; ++e) {
             const int i = threadIdx.x + e * BLOCK;
             if (i >= count || l.at[i] < from || l.at[i] >= to) continue;
+            const int mine = l.at[i];
             bool first = true;
             float add = 0.f;
-            for (int j = 0; j < count; ++j)
-                if (l.at[j] == l.at[i]) {
-                    if (j < i) first = false;
-                    add += l.add[j];
-                }
+            for (int j = 0; j < count; j += 4) {
+                const int4 at = *reinterpret_cast<const int4 *>(l.at + j);
+                const float4 a = *reinterpret_cast<const float4 *>(l.add + j);
+                first &= (at.x != mine || j >= i) & (at.y != mine || j + 1 >= i) & (at.z != mine || j + 2 >= i) & (at.w != mine || j + 3 >= i);
+                add += at.x == mine ? a.x : 0.f;
+                add += at.y == mine ? a.y : 0.f;
+                add += at.z == mine ? a.z : 0.f;
+                add += at.w == mine ? a.w : 0.f;
+            }
             if (first) set_element(out + l.at[i], value(x[e]) + add);
         }
     }
@@ -690,9 +700,11 @@ __global__ __launch_bounds__(BLOCK) void logprob_backward_kernel(const T *logits
         }
     } else {
         for (int i = threadIdx.x; i < given; i += BLOCK) {
-            l.at[i] = targets[r * given + i];
-            l.add[i] = gradient(l.at[i], dlogprob[r * given + i]);
+            const int64_t at = targets[r * given + i];
+            l.at[i] = at < n ? (int)(at < 0 ? -1 : at) : -1;
+            l.add[i] = gradient(at, dlogprob[r * given + i]);
         }
+        l.close(given);
         __syncthreads();
         for (int i = 0; i < given; ++i) all += l.add[i];
     }
@@ -831,10 +843,10 @@ template <int BLOCK> __device__ __forceinline__ Entries read_entries(const Disti
         int64_t at = d.index[r * d.kept + i];
         const float t = d.teacher[r * d.kept + i];
         if (t == -INFINITY) at = -1;
-        if (at >= n) v[1] = 1.f;
+        if (at >= n) v[1] = 1.f, at = -1;
         if (at >= 0 && !(t < INFINITY)) v[1] = 1.f;
         if (at >= 0) v[0] = fmaxf(v[0], t);
-        l.at[i] = at;
+        l.at[i] = at < 0 ? -1 : (int)at;
         l.add[i] = t;
     }
     block_join<BLOCK>(v, lds, Max());
@@ -860,7 +872,7 @@ __device__ __forceinline__ float row_loss(const DistillArgs &d, const T *row, in
         // T ln q and T ln p, which stay in range where ln p itself would not (a class masked with the type's lowest value, T < 1)
         const float tlns = d.temperature * logf(a.s), tlnsum = d.temperature * e.lnsum;
         for (int i = threadIdx.x; i < d.kept; i += BLOCK) {
-            if (l.at[i] < 0 || l.at[i] >= n) continue;
+            if (l.at[i] < 0) continue;
             const float lnq = l.add[i] - e.max - tlnsum, q = exp2_fast(lnq * (inv_t * LOG2E));
             const float lnp = none ? -INFINITY : element(row + l.at[i]) - a.m - tlns;
             if (!(q == 0.f)) sum[0] += q * (lnq - lnp);
@@ -893,13 +905,14 @@ template <int BLOCK, bool TWO> __device__ __forceinline__ Coefs row_coefs(const 
     if (d.labels != nullptr && d.alpha < 1.f) {
         const int64_t at = d.labels[r];
         if (threadIdx.x == 0) {
-            l.at[d.kept] = at < n ? at : -1;
+            l.at[d.kept] = at >= 0 && at < n ? (int)at : -1;
             l.add[d.kept] = none ? 0.f : -hard;
         }
         ++k.count;
         if (at >= 0 && !none) k.c1 = hard / (TWO ? s1 : s);
         if (at >= n) k.c1 = NAN;
     }
+    l.close(k.count);
     __syncthreads();
     return k;
 }
