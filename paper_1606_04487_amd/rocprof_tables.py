@@ -49,7 +49,8 @@ def kernel_class(name: str):
                      ("reduce_partials", "reduce_partials"), ("reduce_wide", "reduce_partials"), ("reduce_store", "reduce_partials"),
                      ("maxpool_fwd", "maxpool_forward"), ("maxpool_bwd", "maxpool_backward"),
                      ("maxpool_forward", "maxpool_forward"), ("maxpool_backward", "maxpool_backward"),
-                     ("relu", "relu"), ("sgd", "sgd"), ("lrn", "lrn"), ("dropout", "dropout")):
+                     ("relu", "relu"), ("sgd", "sgd"), ("lrn", "lrn"), ("dropout", "dropout"), ("layer_norm", "layer_norm"), ("distill", "distill"),
+                     ("logprob", "logprob")):
         if key in name:
             return cls
     return None
