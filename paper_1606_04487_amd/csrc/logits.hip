@@ -402,14 +402,25 @@ struct TopOut {
 // ------------------------------------------------------------------------------------------------ few long rows
 // Where there are fewer rows than the chip has room for, a long row is cut into PARTS_MOST parts (fewer, if they would be shorter
 // than PART_LEAST chunks), each a row of its own to one workgroup: one compute unit takes 28 GB/s from memory (a row of 131072
-// bf16: 9 us).  The next launch joins the parts' sums, in their order, and their largest elements.
-constexpr int PART_LEAST = 1024, PARTS_MOST = 64, SPLIT_ROWS = 512, SPLIT_CHUNKS = 4096;
+// bf16: 9 us).  The next launch joins the parts' sums, in their order, and their largest elements.  Sums alone gain up to 512 rows
+// (loss of 400 x 131072 bf16: 22 us in parts, 29 whole; 511: 27 and 31).  Largest elements are looked for once a part, so fewer rows
+// gain, the fewer the shorter they are (5 of 160 x 131072 bf16: 21 and 28, of 400: 38 and 35; of 48 x 50021: 13 and 15, of 256: 19 and 16).
+// Loss and gradient read a whole row once and its parts twice (48 x 131072 bf16: 16 and 24; 160: 30 and 28).
+constexpr int PART_LEAST = 1024, PARTS_MOST = 64, SPLIT_CHUNKS = 4096;
 struct Parts { int count; int64_t length; };  // elements of a part, a multiple of 64; count = 1: the rows are not split
+enum Wanted { SUMS, TOPS, BOTH };
 
-static Parts row_parts(int dtype, int64_t rows, int64_t classes)
+// rows from which on they are not split
+static int64_t split_rows(int64_t chunks, Wanted w)
 {
-    const int64_t v = 16 / (int64_t)elem_size(dtype), chunks = classes / v;
-    if (rows >= SPLIT_ROWS || chunks <= SPLIT_CHUNKS) return {1, classes};
+    if (chunks <= SPLIT_CHUNKS) return 0;
+    return w == SUMS ? 512 : w == BOTH ? 96 : chunks / 64 < 384 ? chunks / 64 : 384;
+}
+
+static Parts row_parts(int dtype, int64_t rows, int64_t classes, Wanted w)
+{
+    const int64_t v = 16 / (int64_t)elem_size(dtype);
+    if (rows >= split_rows(classes / v, w)) return {1, classes};
     int64_t length = round_up((classes + PARTS_MOST - 1) / PARTS_MOST, 64);
     if (length < PART_LEAST * v) length = PART_LEAST * v;
     return {(int)((classes + length - 1) / length), length};
@@ -418,9 +429,9 @@ static Parts row_parts(int dtype, int64_t rows, int64_t classes)
 // bytes of the parts' sums, and of their keys behind them
 static size_t parts_bytes(int dtype, int64_t rows, int64_t classes, int top)
 {
-    const Parts p = row_parts(dtype, 1, classes);
-    const int64_t most = rows < SPLIT_ROWS ? rows : SPLIT_ROWS - 1;  // more rows are not split: a workspace for them serves fewer that are
-    return p.count > 1 ? (size_t)most * p.count * (sizeof(float4) + (size_t)top * sizeof(uint64_t)) : 0;
+    const Wanted w = top > 0 ? TOPS : SUMS;
+    const int64_t from = split_rows(classes / (16 / (int64_t)elem_size(dtype)), w), most = rows < from ? rows : from - 1;  // a workspace for more rows serves fewer
+    return from > 0 ? (size_t)most * row_parts(dtype, 0, classes, w).count * (sizeof(float4) + (size_t)top * sizeof(uint64_t)) : 0;
 }
 size_t logprob_workspace(int dtype, int64_t rows, int64_t classes, int top) { return parts_bytes(dtype, rows, classes, top); }
 size_t distill_workspace(int dtype, int64_t rows, int64_t classes) { return parts_bytes(dtype, rows, classes, 0); }
@@ -793,7 +804,7 @@ template <typename T, bool ENTROPY> static int logprob_forward(const LogitsArgs 
 {
     const int64_t chunks = a.classes / CHUNK<T>;
     const float inv_t = 1.f / a.temperature, c = LOG2E / a.temperature;
-    const Parts p = row_parts(a.dtype, a.rows, a.classes);
+    const Parts p = row_parts(a.dtype, a.rows, a.classes, o.top > 0 ? TOPS : SUMS);
     if (p.count > 1) {
         float4 *sums = (float4 *)workspace;
         uint64_t *keys = (uint64_t *)(sums + a.rows * p.count);
@@ -1074,7 +1085,7 @@ template <typename T> static int distill_loss(const LogitsArgs &a, const Distill
 {
     const float c = distill_scale(d);
     const int64_t chunks = a.classes / CHUNK<T>;
-    const Parts p = row_parts(a.dtype, a.rows, a.classes);
+    const Parts p = row_parts(a.dtype, a.rows, a.classes, SUMS);
     if (p.count > 1) {
         float4 *sums = (float4 *)workspace;
         int st = OMNI_OK;
@@ -1122,7 +1133,7 @@ template <typename T> static int distill_both(const LogitsArgs &a, const Distill
 {
     const float c = distill_scale(d);
     const int64_t chunks = a.classes / CHUNK<T>;
-    const Parts p = row_parts(a.dtype, a.rows, a.classes);
+    const Parts p = row_parts(a.dtype, a.rows, a.classes, BOTH);
     if (p.count > 1) {
         float4 *sums = (float4 *)workspace;
         int st = OMNI_OK;

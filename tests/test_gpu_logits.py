@@ -123,7 +123,7 @@ def test_logprob_lengths(B, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("rows,n", [(1, 32769), (5, 65541), (2, 700001), (511, 33000), (512, 33000)])
+@pytest.mark.parametrize("rows,n", [(1, 32769), (5, 65541), (2, 700001), (511, 33000), (512, 33000), (63, 33000), (64, 33000), (95, 33000), (96, 33000)])
 def test_few_long_rows_in_parts(B, rows, n, dtype):
     # parts that end inside a chunk, more parts than a row may have, and both sides of the number of rows that are split; rows
     # whose largest elements lie in one part, in ties across all parts, and parts without any possible class
