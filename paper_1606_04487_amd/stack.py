@@ -316,7 +316,8 @@ class ConvStack:
                      labels: Optional[torch.Tensor], lr: float, momentum: float, weight_decay: float = 0.0, temperature: float = 1.0,
                      alpha: float = 1.0) -> torch.Tensor:
         """One training step on the mean over the batch of the distillation loss (binding.distill_forward; alpha = 0 and no teacher:
-        the labels' cross entropy): forward, loss and its gradient, backward, update.  Returns the loss of every image."""
+        the labels' cross entropy): forward, loss and its gradient, backward, update.  Returns the loss of every image, in a buffer
+        that the next step writes again."""
         logits = self.logits(self.forward(X))
         N = logits.shape[0]
         if self.d_logits is None:
