@@ -489,3 +489,29 @@ def test_large_gradients_are_those_of_their_rows(B, extra):
         d = B.logprob_backward(part, st[s].clone(), labels[s].clone(), w[s].clone(), w[s].clone(), h[s].clone())
         assert torch.equal(d, out[2][s])
     assert all(untouched(t, extra, 3.0) for t in out)
+
+
+def test_shapes_and_what_the_binding_refuses(B):
+    x = torch.randn(2, 3, 50, device="cuda")
+    t = torch.randint(0, 50, (2, 3), device="cuda")
+    lp, h, index, best, stats = B.logprob_forward(x, t, top=4)
+    assert lp.shape == h.shape == (2, 3) and index.shape == best.shape == (2, 3, 4) and stats.shape == (2, 3, 2)
+    flat = B.logprob_forward(x.view(6, 50), t.view(6), top=4)
+    assert all(torch.equal(a.reshape(b.shape), b) for a, b in zip((lp, h, index, best, stats), flat))
+    loss, grad = B.distill_forward_backward(x, index, best, t, 2.0, 0.5)
+    assert loss.shape == (2, 3) and grad.shape == x.shape
+    ones = torch.ones(2, 3, device="cuda")
+    long = torch.randn(2, 131072, device="cuda")
+    small = torch.empty(16, dtype=torch.uint8, device="cuda")
+    for call in (lambda: B.logprob_forward(x, t.int()), lambda: B.logprob_forward(x, t.cpu()), lambda: B.logprob_forward(x, t.view(-1)[:4]),
+                 lambda: B.logprob_forward(x[:, :1].expand(2, 3, 50), t), lambda: B.logprob_forward(x, t, top=65), lambda: B.logprob_forward(x, t, temperature=0.0),
+                 lambda: B.logprob_forward(x.half(), t), lambda: B.logprob_forward(x.transpose(1, 2), None),
+                 lambda: B.logprob_forward(long, None, top=5, workspace=small),
+                 lambda: B.logprob_backward(x, stats, t, None), lambda: B.logprob_backward(x, stats.view(-1)[:6], t, ones),
+                 lambda: B.logprob_backward(x, stats, t, ones, dentropy=ones), lambda: B.logprob_backward(x, stats, t, ones, dlogits=torch.empty(5, 50, device="cuda")),
+                 lambda: B.distill_forward(x, index, best[..., :3].contiguous(), t, 2.0, 0.5), lambda: B.distill_forward(x, index, None, t, 2.0, 0.5),
+                 lambda: B.distill_forward(x, None, None, t), lambda: B.distill_forward(x, index, best, t.int(), 2.0, 0.5),
+                 lambda: B.distill_forward(x, index, best, t, 2.0, 1.5), lambda: B.distill_forward(long, None, None, t[:, 0].contiguous(), alpha=0.0, workspace=small),
+                 lambda: B.distill_backward(x, index, best, t, 2.0, 0.5, stats=stats), lambda: B.distill_forward_backward(x, index, best, t, 2.0, 0.5, dloss=ones[:1])):
+        with pytest.raises((ValueError, B.OmniError)):
+            call()
