@@ -280,7 +280,7 @@ __global__ __launch_bounds__(1024, 4) void layer_norm_backward_kernel(NormBackwa
     constexpr int AHEAD = WEIGHTS && V == 4 && CHUNKS == 1 ? 2 : 1;
     Raw<T> nx[AHEAD][CHUNKS], nd[AHEAD][CHUNKS];
     float nmu[AHEAD], nrs[AHEAD];
-    auto fetch = [&](int i, int64_t r) {  // (of a row past the last one nothing is used)
+    auto fetch = [&](int i, int64_t r) {  // (a row past the last one is not loaded; settle makes zeros of what the registers hold)
         if (r >= a.rows) return;
         nmu[i] = a.mean[r];
         nrs[i] = a.rstd[r];
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(1024, 4) void layer_norm_backward_kernel(NormBackwa
     for (int turn = 0;; turn ^= 1, r += step) {
         float xh[CHUNKS][V], d[CHUNKS][V], s[2] = {0.f, 0.f};
         const float mu = nmu[0], rs = nrs[0];
-        const int n = r < a.rows ? a.n : 0;  // a row past the last one is zeros, which add nothing
+        const int n = r < a.rows ? a.n : 0;  // a row past the last one has no elements: zeros, which add nothing
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             settle<FIT>(nx[0][c], (c * TEAM + lane) * V, n);

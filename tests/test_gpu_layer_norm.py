@@ -257,3 +257,20 @@ def test_large_gradients_are_those_of_their_rows(B, dtype, rows, width):
     for s in (slice(0, half), slice(half, rows)):
         part, _, _ = B.layer_norm_backward(x[s].clone(), dy[s].clone(), mean[s].clone(), rstd[s].clone(), gamma)
         assert torch.equal(part, dx[s])
+
+
+def whole_numbers(rows, width, dtype, seed=1):
+    """x, dy of small whole numbers, mean 0 and rstd 1 given: xh = x, and every sum of dy and dy xh below 2^24 is exact in any order."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x, dy = (torch.randint(-3, 4, (rows, width), generator=g, device="cuda").to(dtype) for _ in range(2))
+    return x, dy, torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows", [2049, 4095, 4097, 4100, 10001, (1 << 20) + 77])
+@pytest.mark.parametrize("width", [1, 2, 3, 5, 7])
+def test_weights_gradients_of_many_narrow_rows(B, width, rows, dtype):
+    # rows narrower than 16 bytes, in numbers that leave some of a workgroup's 16 teams, and whole workgroups, without a row
+    x, dy, mean, rstd = whole_numbers(rows, width, dtype)
+    _, dgamma, dbeta = B.layer_norm_backward(x, dy, mean, rstd)
+    assert torch.equal(dbeta.double(), dy.double().sum(0)) and torch.equal(dgamma.double(), (dy.double() * x.double()).sum(0))
