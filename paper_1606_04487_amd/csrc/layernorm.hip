@@ -114,6 +114,19 @@ __global__ __launch_bounds__(BLOCK, BLOCK <= 512 ? (FIT == CUT && BLOCK == 512 ?
 // beyond them is read three times, the second and third time from the caches.
 constexpr int LONG_KEPT = 8;
 
+// A thread's sum over its chunks of such a row, chunks of a row of 2^24 fp32 elements being 4096: 64 of them at a time, so that no
+// value is one of 2^14 in a row whose roundings may all go the same way (0.1 in each of 2^24 columns, in one row: a mean of 0.099985).
+struct LongSum {
+    float whole = 0.f, part = 0.f;
+    int count = 0;
+    __device__ __forceinline__ void operator+=(float chunk)
+    {
+        part += chunk;
+        if (++count % 64 == 0) whole += part, part = 0.f;
+    }
+    __device__ __forceinline__ float total() const { return whole + part; }
+};
+
 template <typename T>
 __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T *x, int64_t ldx, int64_t rows, int n, float eps, const float *__restrict__ gamma,
                                                                        const float *__restrict__ beta, T *y, int64_t ldy, float *__restrict__ mean, float *__restrict__ rstd)
@@ -125,7 +138,7 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T *
     const T *row = x + r * ldx;
     const int first = threadIdx.x * V;
     Raw<T> kept[LONG_KEPT];
-    float sum[1] = {0.f}, sq[1] = {0.f};
+    LongSum all, squares;
 #pragma unroll
     for (int c = 0; c < LONG_KEPT; ++c) kept[c] = load_raw<CUT>(row, first + c * STEP, n);
     // f(v, at) for every chunk of the thread that begins inside the row, zero outside it
@@ -145,18 +158,24 @@ __global__ __launch_bounds__(1024) void layer_norm_forward_long_kernel(const T *
 #pragma unroll
     for (int c = 0; c < LONG_KEPT; ++c) settle<CUT>(kept[c], first + c * STEP, n);
     each([&](float(&v)[V], int) {
+        float q = 0.f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum[0] += v[j];
+        for (int j = 0; j < V; ++j) q += v[j];
+        all += q;
     });
+    float sum[1] = {all.total()};
     team_join<1024>(sum, lds[0]);
     const float mu = sum[0] / (float)n;
     each([&](float(&v)[V], int at) {
+        float q = 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const float d = at + j < n ? v[j] - mu : 0.f;
-            sq[0] += d * d;
+            q += d * d;
         }
+        squares += q;
     });
+    float sq[1] = {squares.total()};
     team_join<1024>(sq, lds[1]);
     const float rs = 1.0f / sqrtf(sq[0] / (float)n + eps);
     if (threadIdx.x == 0) {
@@ -397,7 +416,7 @@ template <typename T> __global__ __launch_bounds__(1024) void layer_norm_backwar
     const float mu = a.mean[r], rs = a.rstd[r];
     const int first = threadIdx.x * V;
     Raw<T> kx[KEPT], kd[KEPT];
-    float s[2] = {0.f, 0.f};
+    LongSum gs, gxs;
 #pragma unroll
     for (int c = 0; c < KEPT; ++c) {
         kx[c] = load_raw<CUT>(xr, first + c * STEP, a.n);
@@ -434,12 +453,16 @@ template <typename T> __global__ __launch_bounds__(1024) void layer_norm_backwar
         settle<CUT>(kd[c], first + c * STEP, a.n);
     }
     each([&](float(&x)[V], float(&d)[V], int) {
+        float q = 0.f, qx = 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            s[0] += d[j];
-            s[1] += d[j] * x[j];
+            q += d[j];
+            qx += d[j] * x[j];
         }
+        gs += q;
+        gxs += qx;
     });
+    float s[2] = {gs.total(), gxs.total()};
     team_join<1024>(s, lds);
     const float mg = s[0] / (float)a.n, mgx = s[1] / (float)a.n;
     each([&](float(&x)[V], float(&d)[V], int at) {

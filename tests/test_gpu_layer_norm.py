@@ -274,3 +274,32 @@ def test_weights_gradients_of_many_narrow_rows(B, width, rows, dtype):
     x, dy, mean, rstd = whole_numbers(rows, width, dtype)
     _, dgamma, dbeta = B.layer_norm_backward(x, dy, mean, rstd)
     assert torch.equal(dbeta.double(), dy.double().sum(0)) and torch.equal(dgamma.double(), (dy.double() * x.double()).sum(0))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_wide_rows_of_nearly_equal_values(B, dtype):
+    # 2^24 columns whose sums' roundings all go the same way: a thread adds 2^14 values.  In fp32 those are 4096 chunks of 4: a sum of
+    # 4, 64 of those, 64 of those, then 6 + 15 joins, 153 roundings with those of the terms; in bf16 fewer.
+    n = 1 << 24
+    g = np.random.default_rng(3)
+    x = torch.full((2, n), 0.1).to(dtype)
+    x[1] = (0.1 + 1e-3 * torch.from_numpy(g.standard_normal(n))).to(dtype)
+    dy = torch.full((2, n), 0.7).to(dtype)
+    dy[1, ::2] = 0.3
+    xg, dyg = x.cuda(), dy.cuda()
+    x, dy = x.double().numpy(), dy.double().numpy()
+    y, mean, rstd = B.layer_norm_forward(xg)
+    ref, rm, rr = ne.layer_norm_forward(x)
+    em = CHAIN * U * np.abs(x).mean(1)
+    er = CHAIN * U + (em * rr) ** 2
+    assert np.all(np.abs(host(mean) - rm) <= em)
+    assert np.all(np.abs(host(rstd) - rr) <= er * rr)
+    xh = np.abs(x - rm[:, None]) * rr[:, None]
+    assert np.all(np.abs(host(y) - ref) <= (xh * er[:, None] + 8 * U * xh + (em * rr)[:, None]) * 1.01 + half_step(dtype) * np.abs(ref) * 1.01)
+    mean, rstd = torch.from_numpy(rm).float().cuda(), torch.from_numpy(rr).float().cuda()
+    dx, _, _ = B.layer_norm_backward(xg, dyg, mean, rstd)
+    ms, rs = host(mean), host(rstd)
+    rdx, _, _ = ne.layer_norm_backward(x, dy, ms, rs)
+    xh, d = np.abs(x - ms[:, None]) * rs[:, None], np.abs(dy)
+    size = rs[:, None] * (d + d.mean(1, keepdims=True) + xh * (d * xh).mean(1, keepdims=True))
+    assert np.all(np.abs(host(dx) - rdx) <= CHAIN * U * size + half_step(dtype) * np.abs(rdx) * 1.01)
