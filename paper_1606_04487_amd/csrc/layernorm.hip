@@ -299,8 +299,13 @@ __global__ __launch_bounds__(1024, 4) void layer_norm_backward_kernel(NormBackwa
     constexpr int AHEAD = WEIGHTS && V == 4 && CHUNKS == 1 ? 2 : 1;
     Raw<T> nx[AHEAD][CHUNKS], nd[AHEAD][CHUNKS];
     float nmu[AHEAD], nrs[AHEAD];
-    auto fetch = [&](int i, int64_t r) {  // (a row past the last one is not loaded; settle makes zeros of what the registers hold)
-        if (r >= a.rows) return;
+    auto fetch = [&](int i, int64_t r) {
+        if (r >= a.rows) {  // not loaded: zeros from settle, which has nothing to say of a TINY chunk
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+                if (FIT == TINY) nx[i][c] = nd[i][c] = {{0, 0, 0, 0}};
+            return;
+        }
         nmu[i] = a.mean[r];
         nrs[i] = a.rstd[r];
 #pragma unroll

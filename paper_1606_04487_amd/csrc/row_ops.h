@@ -78,7 +78,8 @@ template <Fit FIT, typename T> __device__ __forceinline__ Raw<T> load_raw(const 
 template <Fit FIT, typename T> __device__ __forceinline__ void settle(Raw<T> &b, int at, int n)
 {
     constexpr int V = CHUNK<T>;
-    if (FIT != CUT) {  // (a TINY chunk is cut already: here, too, nothing is left of it where the row has no elements)
+    if (FIT == TINY) return;
+    if (FIT == WHOLE) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) b.w[j] = at < n ? b.w[j] : 0;
         return;
