@@ -378,8 +378,9 @@ int omni_dropout_backward(int32_t dtype, int64_t count, float p, uint64_t seed, 
  *       and gradient NaN.  A row with no possible class (all -inf) has loss +inf, where a term is there, and gradient 0.
  *       stats (fp32 [rows][4], nullable) receives what the backward pass needs.
  *   distill_backward: dlogits[i] = w ( alpha T (p_i - sum_{k: index_k = i} q_k) + (1 - alpha) (p1_i - [i = label]) ),
- *       w = scale * dloss[row] (dloss fp32 [rows], nullable: 1), without the terms that the loss is without.  dlogits may be
- *       logits.
+ *       w = scale * dloss[row] (dloss fp32 [rows], nullable: 1), without the terms that the loss is without; a row without
+ *       either term has loss 0 and gradient 0, whatever its logits are.  A NaN or +inf among another row's classes makes its
+ *       loss and gradient NaN.  dlogits may be logits.
  *   distill_forward_backward: both, reading a row once from memory.  dlogits may be logits.
  * Workspaces as the *_workspace_bytes calls say (host only; 0: NULL will do): few long rows are worked on in parts.
  */

@@ -901,14 +901,15 @@ __device__ __forceinline__ float row_loss(const DistillArgs &d, const T *row, in
     return loss;
 }
 
-// The gradient's coefficients: d x = cT 2^(zT) + c1 2^(z1) + what is listed (entries, then the label).
-struct Coefs { float ct, c1; int count; };
+// The gradient's coefficients: d x = cT 2^(zT) + c1 2^(z1) + what is listed (entries, then the label).  idle: the row has neither an
+// entry nor a label, and so no gradient, whatever its logits are (a row that fills a batch up may hold NaN).
+struct Coefs { float ct, c1; int count; bool idle; };
 
 template <int BLOCK, bool TWO> __device__ __forceinline__ Coefs row_coefs(const DistillArgs &d, int64_t r, int n, float m, float s, float s1, const Entries &e, float w, EntryLds &l)
 {
     const float inv_t = 1.f / d.temperature, soft = d.alpha * d.temperature * w, hard = (1.f - d.alpha) * w;
     const bool none = m == -INFINITY && s == 0.f;
-    Coefs k = {0.f, 0.f, d.kept};
+    Coefs k = {0.f, 0.f, d.kept, !e.any && !e.bad};
     for (int i = threadIdx.x; i < d.kept; i += BLOCK)
         l.add[i] = none || l.at[i] < 0 ? 0.f : -soft * exp2_fast(((l.add[i] - e.max) * inv_t - e.lnsum) * LOG2E);
     if (e.any && !none) k.ct = soft / s;
@@ -922,6 +923,7 @@ template <int BLOCK, bool TWO> __device__ __forceinline__ Coefs row_coefs(const 
         ++k.count;
         if (at >= 0 && !none) k.c1 = hard / (TWO ? s1 : s);
         if (at >= n) k.c1 = NAN;
+        if (at >= 0) k.idle = false;
     }
     l.close(k.count);
     __syncthreads();
@@ -986,6 +988,12 @@ __global__ __launch_bounds__(JOIN_BLOCK) void distill_join_kernel(const T *__res
     write_loss<T, JOIN_BLOCK, ALSO>(d, logits + r * ld, r, n, a, loss, stats, l, lds);
 }
 
+// The gradient of an idle row.
+template <typename T, int BLOCK> __device__ __forceinline__ void write_nothing(const T *in, T *out, int n, int64_t c0, int64_t c1, bool past)
+{
+    write_row<T, BLOCK, 1>(in, out, n, c0, c1, past, [](float) { return 0.f; }, [](int, float(&)[CHUNK<T>]) {});
+}
+
 // Loss and gradient of whole rows.  The row's first KEPT chunks a thread stay in registers from the sums to the gradient; what
 // a longer row has beyond them is read again.
 template <typename T, int BLOCK, int KEPT, int ALSO>
@@ -1004,6 +1012,7 @@ __global__ __launch_bounds__(BLOCK) void distill_both_kernel(const T *logits, in
     const Sums a = row_sums<T, BLOCK, ALSO, false, KEPT>(row, n, sp, c, nullptr, lds, kept);
     const Entries e = write_loss<T, BLOCK, ALSO>(d, row, r, n, a, loss, nullptr, l, lds);
     const Coefs k = row_coefs<BLOCK, ALSO != NOTHING>(d, r, n, a.m, a.s, a.t, e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
+    if (k.idle) return write_nothing<T, BLOCK>(row, to, n, 0, (n + 2 * V) / V, past);
     const Gradient<ALSO> value(k, a.m, c);
     ListedOut<T, BLOCK, KEPT_MOST + 1> listed;
     listed.read(row, n, l, k.count);
@@ -1052,6 +1061,7 @@ __global__ __launch_bounds__(BLOCK) void distill_backward_kernel(const T *logits
         __syncthreads();
     }
     const Coefs k = row_coefs<BLOCK, ALSO != NOTHING>(d, r, n, a.m, a.s, a.t, e, d.scale * (d.dloss != nullptr ? d.dloss[r] : 1.f), l);
+    if (k.idle) return write_nothing<T, BLOCK>(in, to, n, c0, c1, pieces.past);
     const Gradient<ALSO> value(k, a.m, c);
     ListedOut<T, BLOCK, KEPT_MOST + 1> listed;
     listed.read(in, to, n, c0, c1, l, k.count);

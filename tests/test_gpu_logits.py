@@ -515,3 +515,27 @@ def test_shapes_and_what_the_binding_refuses(B):
                  lambda: B.distill_backward(x, index, best, t, 2.0, 0.5, stats=stats), lambda: B.distill_forward_backward(x, index, best, t, 2.0, 0.5, dloss=ones[:1])):
         with pytest.raises((ValueError, B.OmniError)):
             call()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n", [(9, 6), (9, 100), (9, 1001), (9, 9001), (9, 40000), (99, 40000)])
+def test_rows_without_a_loss_have_no_gradient(B, rows, n, dtype):
+    # the rows that fill a batch up: no entries and no label, whatever their logits are (parts of a row, and whole rows)
+    x = logits(rows, n, dtype, seed=n)
+    inf, nan = float("inf"), float("nan")
+    x[0, n // 2] = nan
+    x[1, 0] = inf
+    x[2] = nan
+    x[3, n - 1], x[3, 1] = inf, nan
+    x[4] = -inf
+    x[5, n // 3] = nan                           # with entries: NaN
+    x[7, n // 3] = nan                           # with a label: NaN where the labels count
+    g = torch.Generator().manual_seed(n)
+    index, values = torch.randint(0, n, (rows, 5), generator=g), torch.randn(rows, 5, generator=g)
+    labels, w = torch.randint(0, n, (rows,), generator=g), torch.rand(rows, generator=g) + 0.5
+    index[:5], index[7] = -1, -1
+    index[1] = 2
+    values[1] = -inf
+    labels[:7] = -1
+    for temperature, alpha, extra in ((2.0, 0.5, 0), (4.0, 0.5, 1), (3.0, 0.5, 0), (2.0, 1.0, 3), (1.0, 0.0, 0)):
+        check_distill(B, x, index.cuda(), values.cuda(), labels.cuda(), w.cuda(), temperature, alpha, extra)
