@@ -25,3 +25,11 @@ def pytest_collection_modifyitems(config, items):
     for item in items:
         if "gpu" in item.keywords:
             item.add_marker(skip)
+
+
+@pytest.fixture(autouse=True)
+def same_draws_in_every_run():
+    """What a test draws from torch's own generators, without a seed of its own, is the same in every run (a GPU's generator starts
+    from a random seed otherwise), so that a failure can be seen again."""
+    import torch
+    torch.manual_seed(0)

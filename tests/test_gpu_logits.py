@@ -539,3 +539,14 @@ def test_rows_without_a_loss_have_no_gradient(B, rows, n, dtype):
     labels[:7] = -1
     for temperature, alpha, extra in ((2.0, 0.5, 0), (4.0, 0.5, 1), (3.0, 0.5, 0), (2.0, 1.0, 3), (1.0, 0.0, 0)):
         check_distill(B, x, index.cuda(), values.cuda(), labels.cuda(), w.cuda(), temperature, alpha, extra)
+
+
+def test_ties_in_many_short_rows(B):
+    # values of a set of four: nearly every row has equal ones among its largest, which rank by index
+    rows, g = (1 << 20) + 5, torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randint(0, 4, (rows, 5), generator=g, device="cuda").float() * 0.5
+    index, best = B.logprob_forward(x, top=3)[2:4]
+    order = torch.arange(5, device="cuda") - 8 * (x * 2).long()          # descending, then ascending by index; no two are equal
+    assert torch.equal(index, order.sort(dim=1).indices[:, :3])
+    full = torch.log_softmax(x.double(), 1)
+    assert float((best - full.gather(1, index)).abs().max()) < 200 * U * 10
