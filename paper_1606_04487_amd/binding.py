@@ -555,34 +555,34 @@ def dropout_backward(dy, p: float, seed: int, stream_id: int = 0, dx=None):
 
 
 # ---------------------------------------------------------------- the end of a network
-# Matrices here are tensors [..., width] whose rows lie evenly spaced, each contiguous: a slice of a wider matrix is one.
+# Matrices here are tensors [..., width] whose rows lie evenly spaced, each contiguous: a slice of a wider matrix is one.  What
+# belongs to the rows is in their order: its axes in front are theirs, or some of either counted together.
 # A call on small matrices is as long as its host side (10 us of it, 3 the launch, when every tensor asked for the current device
 # and its shape several times), so each tensor is looked at once.
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _f32, _int64 = torch.float32, torch.int64
 
 
-def _device(t: torch.Tensor, what: str) -> int:
-    """The current GPU's number, where `t` has to live."""
-    if not t.is_cuda:
+def _matrix(t: torch.Tensor, dev: Optional[int], what: str):
+    """(data_ptr, rows, width, ld, lead, dev) of a tensor on the current GPU, whose number is dev (None: not known yet).  lead: the
+    rows' shape where they have several axes, else None."""
+    at = t.get_device()
+    if at < 0:
         raise ValueError(f"{what} must live on the GPU")
-    return _current_device()
-
-
-def _matrix(t: torch.Tensor, dev: int, what: str):
-    """(data_ptr, rows, width, ld) of a tensor on the current GPU."""
-    if t.get_device() != dev:
+    if dev is None:
+        dev = _current_device()
+    if at != dev:
         raise ValueError(f"{what} must live on the current GPU")
     if t.dim() == 2:
         rows, width = t.shape
         ld, step = t.stride()
         if step == 1 and (ld >= width or rows < 2) and width > 0:
-            return t.data_ptr(), rows, width, ld if ld >= width else width
+            return t.data_ptr(), rows, width, ld if ld >= width else width, None, dev
     if t.dim() == 0 or t.shape[-1] == 0:
         raise ValueError(f"{what} must have rows of at least one element")
-    width = t.shape[-1]
+    width, lead = t.shape[-1], t.shape[:-1] if t.dim() > 2 else None
     if t.is_contiguous():
-        return t.data_ptr(), t.numel() // width, width, width
+        return t.data_ptr(), t.numel() // width, width, width, lead, dev
     if width > 1 and t.stride(-1) != 1:
         raise ValueError(f"{what} must have contiguous rows")
     rows, ld = 1, None
@@ -596,24 +596,49 @@ def _matrix(t: torch.Tensor, dev: int, what: str):
         rows *= n
     if ld is not None and rows and ld < width:
         raise ValueError(f"{what} must have rows that do not overlap")
-    return t.data_ptr(), rows, width, width if ld is None else max(ld, width)
+    return t.data_ptr(), rows, width, width if ld is None else max(ld, width), lead, dev
 
 
-def _vector(t: Optional[torch.Tensor], count: int, dtype: torch.dtype, dev: int, what: str) -> Optional[int]:
-    """data_ptr of a dense tensor of `count` elements on the current GPU (None stays None)."""
+def _check_order(lead, shape, what: str) -> None:
+    """A tensor of that shape holds what belongs to rows of the shape `lead`, in their order: one's axes are the other's, some of them
+    counted together.  [S, B] beside rows of [B, S] is as many values in another order."""
+    rows = lead.numel()
+    if shape[0] == rows:
+        return
+
+    def ends(s):
+        n, at = 1, {1}
+        for k in s:
+            n *= k
+            if n > rows or n == 0:
+                break
+            at.add(n)
+        return at
+    a, b = ends(lead), ends(shape)
+    if rows and not (a <= b or b <= a):
+        raise ValueError(f"{what} {tuple(shape)} is not in the order of the rows {tuple(lead)}")
+
+
+def _vector(t: Optional[torch.Tensor], count: int, dtype: torch.dtype, dev: int, what: str, lead=None) -> Optional[int]:
+    """data_ptr of a dense tensor of `count` elements on the current GPU (None stays None); with rows of several axes, of one in their
+    order."""
     if t is None:
         return None
     if t.dtype is not dtype or t.numel() != count:
         raise ValueError(f"{what} must be {dtype} and hold {count} elements")
     if t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous and live on the current GPU")
+    if lead is not None and t.shape != lead and t.dim() > 1 and t.shape[:len(lead)] != lead:
+        _check_order(lead, t.shape, what)
     return t.data_ptr()
 
 
-def _like(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, dev: int, what: str):
-    p, r, w, ld = _matrix(t, dev, what)
+def _like(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, dev: int, what: str, lead=None):
+    p, r, w, ld, axes, _ = _matrix(t, dev, what)
     if r != rows or w != width or t.dtype is not dtype:
         raise ValueError(f"{what} must be {dtype} with {rows} rows of {width}")
+    if lead is not None and axes is not None and axes != lead:
+        _check_order(lead, axes, what)
     return p, ld
 
 
@@ -660,31 +685,31 @@ def _scratch(need: int, workspace: Optional[torch.Tensor], dev: int, device):
 def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, y=None, mean=None, rstd=None, want_stats: bool = True):
     """omni_layer_norm_forward over x's last axis; returns (y, mean, rstd) -- mean and rstd (fp32, one a row) are what
     layer_norm_backward needs (None without want_stats, unless they are given)."""
-    dev, dtype = _device(x, "x"), x.dtype
-    px, rows, width, ldx = _matrix(x, dev, "x")
+    dtype = x.dtype
+    px, rows, width, ldx, lead, dev = _matrix(x, None, "x")
     if y is None:
         y = torch.empty(x.shape, dtype=dtype, device=x.device)
-    py, ldy = _like(y, rows, width, dtype, dev, "y")
+    py, ldy = _like(y, rows, width, dtype, dev, "y", lead)
     if want_stats:
         if mean is None:
             mean = torch.empty(x.shape[:-1], dtype=_f32, device=x.device)
         if rstd is None:
             rstd = torch.empty(x.shape[:-1], dtype=_f32, device=x.device)
     _check(_lib.omni_layer_norm_forward(dtype_code(dtype), rows, width, px, ldx, _vector(gamma, width, _f32, dev, "gamma"),
-                                        _vector(beta, width, _f32, dev, "beta"), eps, py, ldy, _vector(mean, rows, _f32, dev, "mean"),
-                                        _vector(rstd, rows, _f32, dev, "rstd"), _stream_of(dev)))
+                                        _vector(beta, width, _f32, dev, "beta"), eps, py, ldy, _vector(mean, rows, _f32, dev, "mean", lead),
+                                        _vector(rstd, rows, _f32, dev, "rstd", lead), _stream_of(dev)))
     return y, mean, rstd
 
 
 def layer_norm_backward(x, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, want_dx: bool = True,
                         want_dweights: bool = True, workspace=None):
     """omni_layer_norm_backward; returns (dx, dgamma, dbeta), dgamma and dbeta fp32 [width]."""
-    dev, dtype = _device(x, "x"), x.dtype
-    px, rows, width, ldx = _matrix(x, dev, "x")
-    pdy, lddy = _like(dy, rows, width, dtype, dev, "dy")
+    dtype = x.dtype
+    px, rows, width, ldx, lead, dev = _matrix(x, None, "x")
+    pdy, lddy = _like(dy, rows, width, dtype, dev, "dy", lead)
     if dx is None and want_dx:
         dx = torch.empty(x.shape, dtype=dtype, device=x.device)
-    pdx, lddx = (None, 0) if dx is None else _like(dx, rows, width, dtype, dev, "dx")
+    pdx, lddx = (None, 0) if dx is None else _like(dx, rows, width, dtype, dev, "dx", lead)
     if want_dweights:
         if dgamma is None:
             dgamma = torch.empty((width,), dtype=_f32, device=x.device)
@@ -693,7 +718,7 @@ def layer_norm_backward(x, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbe
     weights = dgamma is not None or dbeta is not None
     pw, nw, workspace = _scratch(layer_norm_workspace_bytes(rows, width, dtype) if weights else 0, workspace, dev, x.device)
     _check(_lib.omni_layer_norm_backward(dtype_code(dtype), rows, width, px, ldx, pdy, lddy, _vector(gamma, width, _f32, dev, "gamma"),
-                                         _vector(mean, rows, _f32, dev, "mean"), _vector(rstd, rows, _f32, dev, "rstd"), pdx, lddx,
+                                         _vector(mean, rows, _f32, dev, "mean", lead), _vector(rstd, rows, _f32, dev, "rstd", lead), pdx, lddx,
                                          _vector(dgamma, width, _f32, dev, "dgamma"), _vector(dbeta, width, _f32, dev, "dbeta"), pw, nw,
                                          _stream_of(dev)))
     return dx, dgamma, dbeta
@@ -706,6 +731,8 @@ def _per_row(t: Optional[torch.Tensor], rows: int, what: str) -> int:
     n = t.numel()
     if n % rows:
         raise ValueError(f"{what} must hold the same number of elements for every row")
+    if n != rows and t.dim() > 1 and t.size(0) != rows:
+        _check_order(torch.Size((rows,)), t.shape, what)
     return n // rows
 
 
@@ -714,8 +741,7 @@ def logprob_forward(logits, targets=None, top: int = 0, temperature: float = 1.0
     """omni_logprob_forward over logits [..., classes]; returns (logprob, entropy, top_index, top_logprob, stats).  targets:
     int64, any number of classes a row; logprob has targets' shape, entropy one value a row, top_index (int64) and top_logprob
     `top` a row; stats is what logprob_backward needs.  What is not asked for is None."""
-    dev = _device(logits, "logits")
-    p, rows, classes, ld = _matrix(logits, dev, "logits")
+    p, rows, classes, ld, lead, dev = _matrix(logits, None, "logits")
     given = _per_row(targets, rows, "targets")
     if logprob is None and targets is not None:
         logprob = torch.empty(targets.shape, dtype=_f32, device=logits.device)
@@ -730,53 +756,60 @@ def logprob_forward(logits, targets=None, top: int = 0, temperature: float = 1.0
         stats = torch.empty(logits.shape[:-1] + (2,), dtype=_f32, device=logits.device)
     pw, nw, workspace = _scratch(logprob_workspace_bytes(rows, classes, top, logits.dtype), workspace, dev, logits.device)
     _check(_lib.omni_logprob_forward(dtype_code(logits.dtype), rows, classes, p, ld, temperature,
-                                     _vector(targets, rows * given, _int64, dev, "targets"), given,
-                                     _vector(logprob, rows * given, _f32, dev, "logprob"), _vector(entropy, rows, _f32, dev, "entropy"), top,
-                                     _vector(top_index, rows * top, _int64, dev, "top_index"),
-                                     _vector(top_logprob, rows * top, _f32, dev, "top_logprob"),
-                                     _vector(stats, 2 * rows, _f32, dev, "stats"), pw, nw, _stream_of(dev)))
+                                     _vector(targets, rows * given, _int64, dev, "targets", lead), given,
+                                     _vector(logprob, rows * given, _f32, dev, "logprob", lead), _vector(entropy, rows, _f32, dev, "entropy", lead), top,
+                                     _vector(top_index, rows * top, _int64, dev, "top_index", lead),
+                                     _vector(top_logprob, rows * top, _f32, dev, "top_logprob", lead),
+                                     _vector(stats, 2 * rows, _f32, dev, "stats", lead), pw, nw, _stream_of(dev)))
     return logprob, entropy, top_index, top_logprob, stats
 
 
 def logprob_backward(logits, stats, targets=None, dlogprob=None, dentropy=None, entropy=None, temperature: float = 1.0, dlogits=None):
     """omni_logprob_backward: gradient w.r.t. the logits, from dlogprob (targets' shape) and dentropy (one a row, with the
     entropy that logprob_forward gave)."""
-    dev, dtype = _device(logits, "logits"), logits.dtype
-    p, rows, classes, ld = _matrix(logits, dev, "logits")
+    dtype = logits.dtype
+    p, rows, classes, ld, lead, dev = _matrix(logits, None, "logits")
     given = _per_row(targets, rows, "targets")
     if dlogits is None:
         dlogits = torch.empty(logits.shape, dtype=dtype, device=logits.device)
-    po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits")
-    _check(_lib.omni_logprob_backward(dtype_code(dtype), rows, classes, p, ld, temperature, _vector(stats, 2 * rows, _f32, dev, "stats"),
-                                      _vector(targets, rows * given, _int64, dev, "targets"), given,
-                                      _vector(dlogprob, rows * given, _f32, dev, "dlogprob"), _vector(dentropy, rows, _f32, dev, "dentropy"),
-                                      _vector(entropy, rows, _f32, dev, "entropy"), po, ldo, _stream_of(dev)))
+    po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits", lead)
+    _check(_lib.omni_logprob_backward(dtype_code(dtype), rows, classes, p, ld, temperature, _vector(stats, 2 * rows, _f32, dev, "stats", lead),
+                                      _vector(targets, rows * given, _int64, dev, "targets", lead), given,
+                                      _vector(dlogprob, rows * given, _f32, dev, "dlogprob", lead), _vector(dentropy, rows, _f32, dev, "dentropy", lead),
+                                      _vector(entropy, rows, _f32, dev, "entropy", lead), po, ldo, _stream_of(dev)))
     return dlogits
 
 
-def _teacher(index, values, labels, rows: int, dev: int):
+def _teacher(index, values, labels, rows: int, dev: int, lead):
     """(index pointer, logits pointer, entries a row, labels pointer)"""
-    kept = _per_row(index, rows, "teacher_index")
-    if (index is None) != (values is None) or (index is not None and index.shape != values.shape):
+    if index is None:
+        if values is not None:
+            raise ValueError("teacher_logits without teacher_index")
+        return None, None, 0, _vector(labels, rows, _int64, dev, "labels", lead)
+    shape = index.shape
+    if values is None or shape != values.shape:
         raise ValueError("teacher_index and teacher_logits must have the same shape")
-    return (_vector(index, rows * kept, _int64, dev, "teacher_index"), _vector(values, rows * kept, _f32, dev, "teacher_logits"), kept,
-            _vector(labels, rows, _int64, dev, "labels"))
+    n = index.numel()
+    kept = n // rows if rows else 0
+    if lead is None and len(shape) > 1 and shape[0] != rows:
+        _check_order(torch.Size((rows,)), shape, "teacher_index")
+    return (_vector(index, rows * kept, _int64, dev, "teacher_index", lead), _vector(values, rows * kept, _f32, dev, "teacher_logits", lead), kept,
+            _vector(labels, rows, _int64, dev, "labels", lead))
 
 
 def distill_forward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0, loss=None,
                     stats=None, want_stats: bool = True, workspace=None):
     """omni_distill_forward over logits [..., classes]; returns (loss, stats): the loss of every row, and what distill_backward
     needs.  Without teacher entries (and alpha = 0) it is the labels' cross entropy."""
-    dev = _device(logits, "logits")
-    p, rows, classes, ld = _matrix(logits, dev, "logits")
-    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows, dev)
+    p, rows, classes, ld, lead, dev = _matrix(logits, None, "logits")
+    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows, dev, lead)
     if loss is None:
         loss = torch.empty(logits.shape[:-1], dtype=_f32, device=logits.device)
     if stats is None and want_stats:
         stats = torch.empty(logits.shape[:-1] + (4,), dtype=_f32, device=logits.device)
     pw, nw, workspace = _scratch(distill_workspace_bytes(rows, classes, logits.dtype), workspace, dev, logits.device)
     _check(_lib.omni_distill_forward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                     _vector(loss, rows, _f32, dev, "loss"), _vector(stats, 4 * rows, _f32, dev, "stats"), pw, nw,
+                                     _vector(loss, rows, _f32, dev, "loss", lead), _vector(stats, 4 * rows, _f32, dev, "stats", lead), pw, nw,
                                      _stream_of(dev)))
     return loss, stats
 
@@ -784,14 +817,14 @@ def distill_forward(logits, teacher_index=None, teacher_logits=None, labels=None
 def distill_backward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0, stats=None,
                      dloss=None, scale: float = 1.0, dlogits=None):
     """omni_distill_backward: gradient w.r.t. the logits of sum(scale * dloss * loss) (dloss: one a row; None: ones)."""
-    dev, dtype = _device(logits, "logits"), logits.dtype
-    p, rows, classes, ld = _matrix(logits, dev, "logits")
-    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows, dev)
+    dtype = logits.dtype
+    p, rows, classes, ld, lead, dev = _matrix(logits, None, "logits")
+    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows, dev, lead)
     if dlogits is None:
         dlogits = torch.empty(logits.shape, dtype=dtype, device=logits.device)
-    po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits")
+    po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits", lead)
     _check(_lib.omni_distill_backward(dtype_code(dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                      _vector(stats, 4 * rows, _f32, dev, "stats"), _vector(dloss, rows, _f32, dev, "dloss"), scale,
+                                      _vector(stats, 4 * rows, _f32, dev, "stats", lead), _vector(dloss, rows, _f32, dev, "dloss", lead), scale,
                                       po, ldo, _stream_of(dev)))
     return dlogits
 
@@ -799,17 +832,17 @@ def distill_backward(logits, teacher_index=None, teacher_logits=None, labels=Non
 def distill_forward_backward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0,
                              dloss=None, scale: float = 1.0, loss=None, dlogits=None, workspace=None):
     """omni_distill_forward_backward: distill_forward and distill_backward in one call; returns (loss, dlogits)."""
-    dev, dtype = _device(logits, "logits"), logits.dtype
-    p, rows, classes, ld = _matrix(logits, dev, "logits")
-    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows, dev)
+    dtype = logits.dtype
+    p, rows, classes, ld, lead, dev = _matrix(logits, None, "logits")
+    pi, pv, kept, pl = _teacher(teacher_index, teacher_logits, labels, rows, dev, lead)
     if loss is None:
         loss = torch.empty(logits.shape[:-1], dtype=_f32, device=logits.device)
     if dlogits is None:
         dlogits = torch.empty(logits.shape, dtype=dtype, device=logits.device)
-    po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits")
+    po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits", lead)
     pw, nw, workspace = _scratch(distill_workspace_bytes(rows, classes, dtype), workspace, dev, logits.device)
     _check(_lib.omni_distill_forward_backward(dtype_code(dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                              _vector(dloss, rows, _f32, dev, "dloss"), scale, _vector(loss, rows, _f32, dev, "loss"), po, ldo,
+                                              _vector(dloss, rows, _f32, dev, "dloss", lead), scale, _vector(loss, rows, _f32, dev, "loss", lead), po, ldo,
                                               pw, nw, _stream_of(dev)))
     return loss, dlogits
 

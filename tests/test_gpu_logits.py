@@ -550,3 +550,29 @@ def test_ties_in_many_short_rows(B):
     assert torch.equal(index, order.sort(dim=1).indices[:, :3])
     full = torch.log_softmax(x.double(), 1)
     assert float((best - full.gather(1, index)).abs().max()) < 200 * U * 10
+
+
+def test_what_belongs_to_the_rows_is_in_their_order(B):
+    """[S][B] beside logits of [B][S][classes] holds as many values and means others."""
+    x = torch.randn(2, 3, 50).cuda()
+    t, w = torch.randint(0, 50, (2, 3)).cuda(), torch.rand(2, 3).cuda()
+    lp, h, index, best, stats = B.logprob_forward(x, t, top=4)
+    turned = lambda v: v.transpose(0, 1).contiguous()
+    for call in (lambda: B.logprob_forward(x, turned(t)), lambda: B.logprob_forward(x, t, logprob=turned(lp)), lambda: B.logprob_forward(x, entropy=turned(h)),
+                 lambda: B.logprob_backward(x, turned(stats), t, w), lambda: B.logprob_backward(x, stats, turned(t), w), lambda: B.logprob_backward(x, stats, t, turned(w)),
+                 lambda: B.logprob_backward(x, stats, t, w, turned(w), h), lambda: B.logprob_backward(x, stats, t, w, w, turned(h)),
+                 lambda: B.distill_forward(x, turned(index), turned(best), t, 2.0, 0.5), lambda: B.distill_forward(x, index, best, turned(t), 2.0, 0.5),
+                 lambda: B.distill_forward(x, index, best, t, 2.0, 0.5, loss=turned(w)), lambda: B.distill_forward_backward(x, index, best, t, dloss=turned(w)),
+                 lambda: B.distill_forward_backward(x, index, best, turned(t), 2.0, 0.5), lambda: B.layer_norm_forward(x, mean=turned(w)),
+                 lambda: B.layer_norm_backward(x, x, turned(w), w), lambda: B.layer_norm_backward(x, x, w, turned(w)),
+                 lambda: B.layer_norm_forward(x, y=turned(x)), lambda: B.layer_norm_backward(x, turned(x), w, w), lambda: B.distill_forward_backward(x, index, best, dlogits=turned(x)),
+                 lambda: B.distill_forward(x.view(6, 50), index.view(6, 4).t().contiguous(), best.view(6, 4).t().contiguous())):
+        with pytest.raises(ValueError):
+            call()
+    # the same rows counted together, or with an axis of one or several targets a row more
+    for same in (t.view(6), t.view(2, 3, 1), t.view(1, 2, 3), t.view(6, 1)):
+        assert torch.equal(B.logprob_forward(x, same)[0].view(2, 3), lp)
+    two = torch.stack([t, t], 2)
+    assert torch.equal(B.logprob_forward(x, two)[0], torch.stack([lp, lp], 2)) and torch.equal(B.logprob_forward(x, two.view(6, 2))[0].view(2, 3, 2), torch.stack([lp, lp], 2))
+    assert torch.equal(B.logprob_forward(x.view(6, 50), t)[0], lp)
+    assert torch.equal(B.layer_norm_forward(x, y=torch.empty(6, 50, device="cuda"))[0], B.layer_norm_forward(x)[0].view(6, 50))

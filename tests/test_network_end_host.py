@@ -141,3 +141,15 @@ def test_binding_refuses_what_is_not_on_the_gpu(B):
                  lambda: B.logprob_backward(x, x), lambda: B.distill_forward(x), lambda: B.distill_backward(x), lambda: B.distill_forward_backward(x)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("lead,shape,ordered", [
+    ((2, 3), (2, 3), True), ((2, 3), (6,), True), ((2, 3), (2, 3, 4), True), ((2, 3), (6, 4), True), ((2, 3), (1, 2, 1, 3), True), ((6,), (2, 3), True), ((6,), (3, 2), True),
+    ((2, 3, 4), (6, 4), True), ((2, 3, 4), (2, 12, 5), True), ((6, 4), (2, 3, 4), True), ((1, 1), (5,), True), ((0, 3), (3, 0), True), ((2, 3), (2, 3, 0), True), ((3, 3), (3, 3), True),
+    ((2, 3), (3, 2), False), ((2, 3), (3, 2, 4), False), ((6,), (4, 6), False), ((2, 3, 4), (2, 4, 3), False), ((2, 3, 4), (8, 3), False), ((6, 4), (8, 3), False)])
+def test_what_belongs_to_rows_is_in_their_order(B, lead, shape, ordered):
+    if ordered:
+        B._check_order(torch.Size(lead), torch.Size(shape), "targets")
+    else:
+        with pytest.raises(ValueError):
+            B._check_order(torch.Size(lead), torch.Size(shape), "targets")
