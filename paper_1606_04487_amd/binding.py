@@ -556,7 +556,8 @@ def dropout_backward(dy, p: float, seed: int, stream_id: int = 0, dx=None):
 
 # ---------------------------------------------------------------- the end of a network
 # Matrices here are tensors [..., width] whose rows lie evenly spaced, each contiguous: a slice of a wider matrix is one.  What
-# belongs to the rows is in their order: its axes in front are theirs, or some of either counted together.
+# belongs to the rows is in their order: its axes in front are theirs, or some of either counted together.  Small inputs (weights,
+# statistics, targets, entries, labels) may lie anywhere; matrices and outputs begin on 16 bytes.
 # A call on small matrices is as long as its host side (10 us of it, 3 the launch, when every tensor asked for the current device
 # and its shape several times), so each tensor is looked at once.
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
@@ -633,6 +634,29 @@ def _vector(t: Optional[torch.Tensor], count: int, dtype: torch.dtype, dev: int,
     return t.data_ptr()
 
 
+class _Copy(ctypes.c_void_p):
+    """Where a tensor's copy lies, on 16 bytes and dense; it lives as long as this does, that is until the call is queued."""
+
+    def __init__(self, t: torch.Tensor):
+        self.tensor = t.detach().clone(memory_format=torch.contiguous_format)
+        super().__init__(self.tensor.data_ptr())
+
+
+def _input(t: Optional[torch.Tensor], count: int, dtype: torch.dtype, dev: int, what: str, lead=None):
+    """_vector of a small tensor that is only read: one that is not dense, or not on 16 bytes as the library takes it (targets from
+    the second token on), is copied on the current stream."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != count:
+        raise ValueError(f"{what} must be {dtype} and hold {count} elements")
+    if t.get_device() != dev:
+        raise ValueError(f"{what} must live on the current GPU")
+    if lead is not None and t.shape != lead and t.dim() > 1 and t.shape[:len(lead)] != lead:
+        _check_order(lead, t.shape, what)
+    p = t.data_ptr()
+    return p if t.is_contiguous() and not p & 15 else _Copy(t)
+
+
 def _like(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, dev: int, what: str, lead=None):
     p, r, w, ld, axes, _ = _matrix(t, dev, what)
     if r != rows or w != width or t.dtype is not dtype:
@@ -695,8 +719,8 @@ def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, y=None, mean
             mean = torch.empty(x.shape[:-1], dtype=_f32, device=x.device)
         if rstd is None:
             rstd = torch.empty(x.shape[:-1], dtype=_f32, device=x.device)
-    _check(_lib.omni_layer_norm_forward(dtype_code(dtype), rows, width, px, ldx, _vector(gamma, width, _f32, dev, "gamma"),
-                                        _vector(beta, width, _f32, dev, "beta"), eps, py, ldy, _vector(mean, rows, _f32, dev, "mean", lead),
+    _check(_lib.omni_layer_norm_forward(dtype_code(dtype), rows, width, px, ldx, _input(gamma, width, _f32, dev, "gamma"),
+                                        _input(beta, width, _f32, dev, "beta"), eps, py, ldy, _vector(mean, rows, _f32, dev, "mean", lead),
                                         _vector(rstd, rows, _f32, dev, "rstd", lead), _stream_of(dev)))
     return y, mean, rstd
 
@@ -717,8 +741,8 @@ def layer_norm_backward(x, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbe
             dbeta = torch.empty((width,), dtype=_f32, device=x.device)
     weights = dgamma is not None or dbeta is not None
     pw, nw, workspace = _scratch(layer_norm_workspace_bytes(rows, width, dtype) if weights else 0, workspace, dev, x.device)
-    _check(_lib.omni_layer_norm_backward(dtype_code(dtype), rows, width, px, ldx, pdy, lddy, _vector(gamma, width, _f32, dev, "gamma"),
-                                         _vector(mean, rows, _f32, dev, "mean", lead), _vector(rstd, rows, _f32, dev, "rstd", lead), pdx, lddx,
+    _check(_lib.omni_layer_norm_backward(dtype_code(dtype), rows, width, px, ldx, pdy, lddy, _input(gamma, width, _f32, dev, "gamma"),
+                                         _input(mean, rows, _f32, dev, "mean", lead), _input(rstd, rows, _f32, dev, "rstd", lead), pdx, lddx,
                                          _vector(dgamma, width, _f32, dev, "dgamma"), _vector(dbeta, width, _f32, dev, "dbeta"), pw, nw,
                                          _stream_of(dev)))
     return dx, dgamma, dbeta
@@ -756,7 +780,7 @@ def logprob_forward(logits, targets=None, top: int = 0, temperature: float = 1.0
         stats = torch.empty(logits.shape[:-1] + (2,), dtype=_f32, device=logits.device)
     pw, nw, workspace = _scratch(logprob_workspace_bytes(rows, classes, top, logits.dtype), workspace, dev, logits.device)
     _check(_lib.omni_logprob_forward(dtype_code(logits.dtype), rows, classes, p, ld, temperature,
-                                     _vector(targets, rows * given, _int64, dev, "targets", lead), given,
+                                     _input(targets, rows * given, _int64, dev, "targets", lead), given,
                                      _vector(logprob, rows * given, _f32, dev, "logprob", lead), _vector(entropy, rows, _f32, dev, "entropy", lead), top,
                                      _vector(top_index, rows * top, _int64, dev, "top_index", lead),
                                      _vector(top_logprob, rows * top, _f32, dev, "top_logprob", lead),
@@ -773,10 +797,10 @@ def logprob_backward(logits, stats, targets=None, dlogprob=None, dentropy=None, 
     if dlogits is None:
         dlogits = torch.empty(logits.shape, dtype=dtype, device=logits.device)
     po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits", lead)
-    _check(_lib.omni_logprob_backward(dtype_code(dtype), rows, classes, p, ld, temperature, _vector(stats, 2 * rows, _f32, dev, "stats", lead),
-                                      _vector(targets, rows * given, _int64, dev, "targets", lead), given,
-                                      _vector(dlogprob, rows * given, _f32, dev, "dlogprob", lead), _vector(dentropy, rows, _f32, dev, "dentropy", lead),
-                                      _vector(entropy, rows, _f32, dev, "entropy", lead), po, ldo, _stream_of(dev)))
+    _check(_lib.omni_logprob_backward(dtype_code(dtype), rows, classes, p, ld, temperature, _input(stats, 2 * rows, _f32, dev, "stats", lead),
+                                      _input(targets, rows * given, _int64, dev, "targets", lead), given,
+                                      _input(dlogprob, rows * given, _f32, dev, "dlogprob", lead), _input(dentropy, rows, _f32, dev, "dentropy", lead),
+                                      _input(entropy, rows, _f32, dev, "entropy", lead), po, ldo, _stream_of(dev)))
     return dlogits
 
 
@@ -785,7 +809,7 @@ def _teacher(index, values, labels, rows: int, dev: int, lead):
     if index is None:
         if values is not None:
             raise ValueError("teacher_logits without teacher_index")
-        return None, None, 0, _vector(labels, rows, _int64, dev, "labels", lead)
+        return None, None, 0, _input(labels, rows, _int64, dev, "labels", lead)
     shape = index.shape
     if values is None or shape != values.shape:
         raise ValueError("teacher_index and teacher_logits must have the same shape")
@@ -793,8 +817,8 @@ def _teacher(index, values, labels, rows: int, dev: int, lead):
     kept = n // rows if rows else 0
     if lead is None and len(shape) > 1 and shape[0] != rows:
         _check_order(torch.Size((rows,)), shape, "teacher_index")
-    return (_vector(index, rows * kept, _int64, dev, "teacher_index", lead), _vector(values, rows * kept, _f32, dev, "teacher_logits", lead), kept,
-            _vector(labels, rows, _int64, dev, "labels", lead))
+    return (_input(index, rows * kept, _int64, dev, "teacher_index", lead), _input(values, rows * kept, _f32, dev, "teacher_logits", lead), kept,
+            _input(labels, rows, _int64, dev, "labels", lead))
 
 
 def distill_forward(logits, teacher_index=None, teacher_logits=None, labels=None, temperature: float = 1.0, alpha: float = 1.0, loss=None,
@@ -824,7 +848,7 @@ def distill_backward(logits, teacher_index=None, teacher_logits=None, labels=Non
         dlogits = torch.empty(logits.shape, dtype=dtype, device=logits.device)
     po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits", lead)
     _check(_lib.omni_distill_backward(dtype_code(dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                      _vector(stats, 4 * rows, _f32, dev, "stats", lead), _vector(dloss, rows, _f32, dev, "dloss", lead), scale,
+                                      _input(stats, 4 * rows, _f32, dev, "stats", lead), _input(dloss, rows, _f32, dev, "dloss", lead), scale,
                                       po, ldo, _stream_of(dev)))
     return dlogits
 
@@ -842,7 +866,7 @@ def distill_forward_backward(logits, teacher_index=None, teacher_logits=None, la
     po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits", lead)
     pw, nw, workspace = _scratch(distill_workspace_bytes(rows, classes, dtype), workspace, dev, logits.device)
     _check(_lib.omni_distill_forward_backward(dtype_code(dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
-                                              _vector(dloss, rows, _f32, dev, "dloss", lead), scale, _vector(loss, rows, _f32, dev, "loss", lead), po, ldo,
+                                              _input(dloss, rows, _f32, dev, "dloss", lead), scale, _vector(loss, rows, _f32, dev, "loss", lead), po, ldo,
                                               pw, nw, _stream_of(dev)))
     return loss, dlogits
 

@@ -576,3 +576,54 @@ def test_what_belongs_to_the_rows_is_in_their_order(B):
     assert torch.equal(B.logprob_forward(x, two)[0], torch.stack([lp, lp], 2)) and torch.equal(B.logprob_forward(x, two.view(6, 2))[0].view(2, 3, 2), torch.stack([lp, lp], 2))
     assert torch.equal(B.logprob_forward(x.view(6, 50), t)[0], lp)
     assert torch.equal(B.layer_norm_forward(x, y=torch.empty(6, 50, device="cuda"))[0], B.layer_norm_forward(x)[0].view(6, 50))
+
+
+def test_small_inputs_that_begin_anywhere(B):
+    """The next-token call: targets one token on, from the middle of their tensor; and inputs that are not contiguous."""
+    rows, n = 33, 301
+    x = logits(rows, n, torch.bfloat16)
+    tokens, far = torch.randint(0, n, (rows + 1,)).cuda(), torch.rand(2 * rows + 3).cuda()
+    odd = lambda t: torch.cat([t.new_zeros(1), t.reshape(-1)])[1:].view(t.shape)  # the same values, one element further on
+    assert all(odd(t).data_ptr() % 16 for t in (tokens, far))
+    t, w = tokens[1:], far[1:rows + 1]
+    want = B.logprob_forward(x, t.clone(), 5)
+    got = B.logprob_forward(x, t, 5)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    lp, h, index, best, stats = want
+    want = B.logprob_backward(x, stats, t.clone(), w.clone(), w.clone(), h)
+    assert torch.equal(B.logprob_backward(x, odd(stats), t, w, torch.stack([w, h], 1)[:, 0], odd(h)), want)
+    wanted = B.distill_forward_backward(x, index, best, t.clone(), 2.0, 0.5, dloss=w.clone())
+    wide, deep = torch.cat([index, index], 1), torch.cat([best, best], 1)
+    loss, d = B.distill_forward_backward(x, wide[:, 5:], deep[:, :5], t, 2.0, 0.5, dloss=w)
+    assert torch.equal(loss, wanted[0]) and torch.equal(d, wanted[1])
+    loss, st = B.distill_forward(x, odd(index), odd(best), t, 2.0, 0.5)
+    assert torch.equal(B.distill_backward(x, odd(index), odd(best), t, 2.0, 0.5, stats=odd(st), dloss=w),
+                       B.distill_backward(x, index, best, t.clone(), 2.0, 0.5, stats=st, dloss=w.clone()))
+    gamma, beta = torch.rand(n).cuda(), torch.rand(n).cuda()
+    y, mean, rstd = B.layer_norm_forward(x, gamma, beta)
+    assert torch.equal(B.layer_norm_forward(x, odd(gamma), odd(beta))[0], y)
+    assert all(torch.equal(a, b) for a, b in zip(B.layer_norm_backward(x, y, odd(mean), odd(rstd), odd(gamma)), B.layer_norm_backward(x, y, mean, rstd, gamma)))
+    # what is written has to lie where the library takes it
+    with pytest.raises(B.OmniError):
+        B.distill_forward(x, index, best, t, 2.0, 0.5, loss=far[1:rows + 1])
+
+
+def test_small_inputs_that_begin_anywhere_in_a_replayed_graph(B):
+    x, tokens = logits(40, 1000, torch.float32), torch.randint(0, 1000, (41,)).cuda()
+    loss, out = torch.empty(40, device="cuda"), torch.empty_like(x)
+
+    def step():
+        B.distill_forward_backward(x, labels=tokens[1:], alpha=0.0, loss=loss, dlogits=out)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        tokens.copy_(torch.randint(0, 1000, (41,)))
+        want = B.distill_forward_backward(x, labels=tokens[1:].clone(), alpha=0.0)
+        loss.zero_(), out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want[0]) and torch.equal(out, want[1])
