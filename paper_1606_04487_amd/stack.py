@@ -67,6 +67,7 @@ class ConvStack:
                                  (B.FLAG_RELU if L.relu else 0) | (B.FLAG_SPLIT_K if L.Ho * L.Wo == 1 else extra))
                      for L in self.layers]
         self.dropout_seed = 1
+        self.dropped = True          # whether the last forward pass had the dropout layers
         self.fwd_fused = [fused and B.conv_fused_supported(d, B.PASS_FORWARD) for d in self.desc]
         self.desc_wgrad = [d.with_flags((B.FLAG_FUSED if ff else B.FLAG_DHAT_CACHED) | (d.flags & B.FLAG_SPLIT_K))
                            for d, ff in zip(self.desc, self.fwd_fused)]
@@ -194,7 +195,8 @@ class ConvStack:
 
     # ------------------------------------------------------------------ passes
     def forward(self, X: torch.Tensor, train: bool = True) -> torch.Tensor:
-        """The output for X.  train = False leaves the dropout layers out."""
+        """The output for X.  train = False leaves the dropout layers out, here and in the backward pass of this forward pass."""
+        self.dropped = train
         cur = X
         for i, L in enumerate(self.layers):
             self.X[i] = cur
@@ -223,7 +225,7 @@ class ConvStack:
         g = dOut
         for i in reversed(range(len(self.layers))):
             L, Y = self.layers[i], self.Y[i]
-            if L.dropout_after > 0:
+            if self.dropped and L.dropout_after > 0:
                 B.dropout_backward(g, L.dropout_after, self.dropout_seed, i, dx=self.gD[i])
                 g = self.gD[i]
             if L.norm_after:

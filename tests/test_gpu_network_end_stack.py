@@ -145,3 +145,20 @@ def test_distill_step_captured_and_replayed(B):
         for a, b in zip(nets[0].W + nets[0].b + [nets[0].loss] + [m.gamma for m in nets[0].norms if m is not None],
                         nets[1].W + nets[1].b + [nets[1].loss] + [m.gamma for m in nets[1].norms if m is not None]):
             assert torch.equal(a, b)
+
+
+def test_backward_of_a_pass_without_dropout(B):
+    """After forward(train=False) backward is the gradient of that pass: nothing was dropped."""
+    from dataclasses import replace
+    from paper_1606_04487_amd.stack import ConvStack
+    plain, dropped = ConvStack(LAYERS, dtype=0), ConvStack([replace(LAYERS[0], dropout_after=0.5)] + LAYERS[1:], dtype=0)
+    Ws, bs = parameters(5)
+    X, d = torch.randn(N, 3, 9, 9).cuda(), torch.randn(N, CLASSES, 1, 1).cuda()
+    for net in (plain, dropped):
+        net.set_parameters(Ws, bs)
+        net.forward(X, train=False)
+        net.backward(d)
+    assert all(torch.equal(a, b) for a, b in zip(plain.dW + plain.db, dropped.dW + dropped.db))
+    dropped.forward(X)
+    dropped.backward(d)
+    assert not torch.equal(plain.dW[0], dropped.dW[0])
