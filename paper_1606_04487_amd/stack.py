@@ -68,6 +68,7 @@ class ConvStack:
                      for L in self.layers]
         self.dropout_seed = 1
         self.dropped = True          # whether the last forward pass had the dropout layers
+        self.answered = False        # whether it was log_probs'
         self.fwd_fused = [fused and B.conv_fused_supported(d, B.PASS_FORWARD) for d in self.desc]
         self.desc_wgrad = [d.with_flags((B.FLAG_FUSED if ff else B.FLAG_DHAT_CACHED) | (d.flags & B.FLAG_SPLIT_K))
                            for d, ff in zip(self.desc, self.fwd_fused)]
@@ -196,7 +197,7 @@ class ConvStack:
     # ------------------------------------------------------------------ passes
     def forward(self, X: torch.Tensor, train: bool = True) -> torch.Tensor:
         """The output for X.  train = False leaves the dropout layers out, here and in the backward pass of this forward pass."""
-        self.dropped = train
+        self.dropped, self.answered = train, False
         cur = X
         for i, L in enumerate(self.layers):
             self.X[i] = cur
@@ -222,6 +223,9 @@ class ConvStack:
         return cur
 
     def backward(self, dOut: torch.Tensor) -> Optional[torch.Tensor]:
+        """The gradients of the last forward pass; the data gradient of the first layer, if it has one."""
+        if self.answered:
+            raise RuntimeError("log_probs has used the buffers that the backward pass reads: call forward again first")
         g = dOut
         for i in reversed(range(len(self.layers))):
             L, Y = self.layers[i], self.Y[i]
@@ -311,8 +315,11 @@ class ConvStack:
 
     def log_probs(self, X: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 5, temperature: float = 1.0):
         """What the network answers for X (without dropout): (logprob, entropy, top_index, top_logprob) of
-        binding.logprob_forward.  The top alternatives are what distill_step takes of a teacher."""
-        return B.logprob_forward(self.logits(self.forward(X, train=False)), targets, top, temperature, want_stats=False)[:4]
+        binding.logprob_forward.  The top alternatives are what distill_step takes of a teacher.  It uses the buffers of the forward
+        pass, so a forward pass before it has no backward pass any more."""
+        out = self.forward(X, train=False)
+        self.answered = True
+        return B.logprob_forward(self.logits(out), targets, top, temperature, want_stats=False)[:4]
 
     def distill_step(self, X: torch.Tensor, teacher_index: Optional[torch.Tensor], teacher_logits: Optional[torch.Tensor],
                      labels: Optional[torch.Tensor], lr: float, momentum: float, weight_decay: float = 0.0, temperature: float = 1.0,
