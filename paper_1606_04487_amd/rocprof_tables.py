@@ -30,7 +30,8 @@ CAL_KIB = 262144.0   # the calibration copy of bench.py: 256 MiB read, 256 MiB w
 
 
 def kernel_class(name: str):
-    """Kernel function name -> the library's timing class (the names omni_profile_kernel_name returns)."""
+    """Kernel function name -> the library's timing class (the names omni_profile_kernel_name returns; "row_parts" where few long rows
+    are read in parts, a launch of log probabilities and of the distillation loss alike, which the library counts with either)."""
     if "fused_conv_kernel" in name or "whole_patch_kernel" in name:
         return "conv_fused"
     if "strided_conv_kernel" in name:
@@ -50,7 +51,7 @@ def kernel_class(name: str):
                      ("maxpool_fwd", "maxpool_forward"), ("maxpool_bwd", "maxpool_backward"),
                      ("maxpool_forward", "maxpool_forward"), ("maxpool_backward", "maxpool_backward"),
                      ("relu", "relu"), ("sgd", "sgd"), ("lrn", "lrn"), ("dropout", "dropout"), ("layer_norm", "layer_norm"), ("distill", "distill"),
-                     ("logprob", "logprob")):
+                     ("logprob", "logprob"), ("row_parts", "row_parts")):
         if key in name:
             return cls
     return None

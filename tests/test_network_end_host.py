@@ -153,3 +153,18 @@ def test_what_belongs_to_rows_is_in_their_order(B, lead, shape, ordered):
     else:
         with pytest.raises(ValueError):
             B._check_order(torch.Size(lead), torch.Size(shape), "targets")
+
+
+@pytest.mark.parametrize("name,cls", [
+    ("void omni::layer_norm_forward_kernel<float, 512, 2, (omni::Fit)0>(float const*, long)", "layer_norm"),
+    ("void omni::layer_norm_backward_long_kernel<unsigned short>(omni::NormBackward<unsigned short>, int)", "layer_norm"),
+    ("omni::layer_norm_join_kernel(float const*, int, int, float*, float*)", "layer_norm"),
+    ("void omni::logprob_forward_kernel<float, 64, 4, true>(float const*, long)", "logprob"), ("void omni::logprob_join_kernel<float, true>(float const*, long)", "logprob"),
+    ("void omni::logprob_backward_kernel<unsigned short, 256, true>(unsigned short const*, long)", "logprob"),
+    ("void omni::row_parts_kernel<unsigned short, 4, 1, true>(unsigned short const*, long)", "row_parts"),
+    ("void omni::distill_loss_kernel<float, 64, 0>(float const*, long)", "distill"), ("void omni::distill_join_kernel<float, 3>(float const*, long)", "distill"),
+    ("void omni::distill_both_kernel<float, 64, 4, 4>(float const*, long)", "distill"), ("void omni::distill_backward_kernel<float, 256, 0>(float const*, long)", "distill"),
+    ("void omni::lrn_forward_kernel<float>(float const*)", "lrn"), ("void at::native::vectorized_elementwise_kernel<4>(int)", None)])
+def test_every_kernel_has_its_class_in_the_tables(name, cls):
+    from paper_1606_04487_amd.rocprof_tables import kernel_class
+    assert kernel_class(name) == cls
