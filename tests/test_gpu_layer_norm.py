@@ -303,3 +303,25 @@ def test_wide_rows_of_nearly_equal_values(B, dtype):
     xh, d = np.abs(x - ms[:, None]) * rs[:, None], np.abs(dy)
     size = rs[:, None] * (d + d.mean(1, keepdims=True) + xh * (d * xh).mean(1, keepdims=True))
     assert np.all(np.abs(host(dx) - rdx) <= CHAIN * U * size + half_step(dtype) * np.abs(rdx) * 1.01)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows", [2049, 4100])
+@pytest.mark.parametrize("width", [8, 255, 256, 300, 512, 777, 1000, 1024, 2000, 2048, 4096, 4100, 8191, 8192])
+def test_weights_gradients_of_every_team(B, width, rows, dtype):
+    # 64 to 1024 threads a row, whole and cut rows; dx beside them, and over x and dy
+    x, dy, mean, rstd = whole_numbers(rows, width, dtype)
+    gamma = torch.randint(1, 4, (width,), device="cuda").float()
+    dx, dgamma, dbeta = B.layer_norm_backward(x, dy, mean, rstd, gamma)
+    assert torch.equal(dbeta.double(), dy.double().sum(0)) and torch.equal(dgamma.double(), (dy.double() * x.double()).sum(0))
+    # the two means are exact sums divided once; a product and two differences behind them, and the rounding on store
+    xd, g = x.double(), dy.double() * gamma.double()
+    mg, mgx = g.mean(1, keepdim=True), (g * xd).mean(1, keepdim=True)
+    ref = g - mg - xd * mgx
+    bound = 6 * U * (g.abs() + mg.abs() + (xd * mgx).abs()) + half_step(dtype) * ref.abs() * 1.01
+    assert bool(((dx.double() - ref).abs() <= bound).all())
+    for over in ("x", "dy"):
+        a, b = x.clone(), dy.clone()
+        to = a if over == "x" else b
+        got = B.layer_norm_backward(a, b, mean, rstd, gamma, dx=to)
+        assert torch.equal(to, dx) and torch.equal(got[1], dgamma) and torch.equal(got[2], dbeta)

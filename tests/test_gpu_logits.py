@@ -627,3 +627,10 @@ def test_small_inputs_that_begin_anywhere_in_a_replayed_graph(B):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(loss, want[0]) and torch.equal(out, want[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n,extra", [(96, 70001, 0), (97, 140003, 1)])
+def test_distill_long_rows_that_are_not_split(B, rows, n, extra, dtype):
+    # workgroups of 1024 that keep a whole row, and rows longer than they keep
+    check_distill(B, logits(rows, n, dtype), *teacher(rows, n, 9, 4), 2.0, 0.5, extra)
