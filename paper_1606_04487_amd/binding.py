@@ -658,6 +658,12 @@ def _input(t: Optional[torch.Tensor], count: int, dtype: torch.dtype, dev: int, 
 
 
 def _like(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, dev: int, what: str, lead=None):
+    """(data_ptr, ld) of a tensor beside that matrix, of its size and type and in its rows' order."""
+    if t.dim() == 2 and t.dtype is dtype and t.get_device() == dev:  # (the ordinary one without another call)
+        r, w = t.shape
+        ld, step = t.stride()
+        if r == rows and w == width and step == 1 and ld >= width:
+            return t.data_ptr(), ld
     p, r, w, ld, axes, _ = _matrix(t, dev, what)
     if r != rows or w != width or t.dtype is not dtype:
         raise ValueError(f"{what} must be {dtype} with {rows} rows of {width}")
@@ -666,8 +672,8 @@ def _like(t: torch.Tensor, rows: int, width: int, dtype: torch.dtype, dev: int, 
     return p, ld
 
 
-def _stream_of(dev: int) -> int:
-    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
+# the current stream's handle on the current GPU
+_stream_of = _raw_stream or (lambda dev: torch.cuda.current_stream().cuda_stream)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -694,13 +700,13 @@ def distill_workspace_bytes(rows: int, classes: int, dtype: torch.dtype = torch.
     return b.value
 
 
-def _scratch(need: int, workspace: Optional[torch.Tensor], dev: int, device):
+def _scratch(need: int, workspace: Optional[torch.Tensor], dev: int, beside: torch.Tensor):
     """(pointer, bytes, tensor) of the caller's workspace, or else of one from torch's allocator, which keeps its memory for the
-    work queued on this stream."""
+    work queued on this stream, on the device of `beside`."""
     if workspace is None:
         if need == 0:
             return None, 0, None
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = torch.empty(need, dtype=torch.uint8, device=beside.device)
         return workspace.data_ptr(), need, workspace
     n = workspace.numel()
     return _vector(workspace, n, workspace.dtype, dev, "workspace"), n * workspace.element_size(), workspace
@@ -740,7 +746,7 @@ def layer_norm_backward(x, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbe
         if dbeta is None:
             dbeta = torch.empty((width,), dtype=_f32, device=x.device)
     weights = dgamma is not None or dbeta is not None
-    pw, nw, workspace = _scratch(layer_norm_workspace_bytes(rows, width, dtype) if weights else 0, workspace, dev, x.device)
+    pw, nw, workspace = _scratch(layer_norm_workspace_bytes(rows, width, dtype) if weights else 0, workspace, dev, x)
     _check(_lib.omni_layer_norm_backward(dtype_code(dtype), rows, width, px, ldx, pdy, lddy, _input(gamma, width, _f32, dev, "gamma"),
                                          _input(mean, rows, _f32, dev, "mean", lead), _input(rstd, rows, _f32, dev, "rstd", lead), pdx, lddx,
                                          _vector(dgamma, width, _f32, dev, "dgamma"), _vector(dbeta, width, _f32, dev, "dbeta"), pw, nw,
@@ -778,7 +784,7 @@ def logprob_forward(logits, targets=None, top: int = 0, temperature: float = 1.0
             top_logprob = torch.empty(logits.shape[:-1] + (top,), dtype=_f32, device=logits.device)
     if stats is None and want_stats:
         stats = torch.empty(logits.shape[:-1] + (2,), dtype=_f32, device=logits.device)
-    pw, nw, workspace = _scratch(logprob_workspace_bytes(rows, classes, top, logits.dtype), workspace, dev, logits.device)
+    pw, nw, workspace = _scratch(logprob_workspace_bytes(rows, classes, top, logits.dtype), workspace, dev, logits)
     _check(_lib.omni_logprob_forward(dtype_code(logits.dtype), rows, classes, p, ld, temperature,
                                      _input(targets, rows * given, _int64, dev, "targets", lead), given,
                                      _vector(logprob, rows * given, _f32, dev, "logprob", lead), _vector(entropy, rows, _f32, dev, "entropy", lead), top,
@@ -831,7 +837,7 @@ def distill_forward(logits, teacher_index=None, teacher_logits=None, labels=None
         loss = torch.empty(logits.shape[:-1], dtype=_f32, device=logits.device)
     if stats is None and want_stats:
         stats = torch.empty(logits.shape[:-1] + (4,), dtype=_f32, device=logits.device)
-    pw, nw, workspace = _scratch(distill_workspace_bytes(rows, classes, logits.dtype), workspace, dev, logits.device)
+    pw, nw, workspace = _scratch(distill_workspace_bytes(rows, classes, logits.dtype), workspace, dev, logits)
     _check(_lib.omni_distill_forward(dtype_code(logits.dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
                                      _vector(loss, rows, _f32, dev, "loss", lead), _vector(stats, 4 * rows, _f32, dev, "stats", lead), pw, nw,
                                      _stream_of(dev)))
@@ -864,7 +870,7 @@ def distill_forward_backward(logits, teacher_index=None, teacher_logits=None, la
     if dlogits is None:
         dlogits = torch.empty(logits.shape, dtype=dtype, device=logits.device)
     po, ldo = _like(dlogits, rows, classes, dtype, dev, "dlogits", lead)
-    pw, nw, workspace = _scratch(distill_workspace_bytes(rows, classes, dtype), workspace, dev, logits.device)
+    pw, nw, workspace = _scratch(distill_workspace_bytes(rows, classes, dtype), workspace, dev, logits)
     _check(_lib.omni_distill_forward_backward(dtype_code(dtype), rows, classes, p, ld, pi, pv, kept, pl, temperature, alpha,
                                               _input(dloss, rows, _f32, dev, "dloss", lead), scale, _vector(loss, rows, _f32, dev, "loss", lead), po, ldo,
                                               pw, nw, _stream_of(dev)))
