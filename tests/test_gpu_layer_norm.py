@@ -325,3 +325,21 @@ def test_weights_gradients_of_every_team(B, width, rows, dtype):
         to = a if over == "x" else b
         got = B.layer_norm_backward(a, b, mean, rstd, gamma, dx=to)
         assert torch.equal(to, dx) and torch.equal(got[1], dgamma) and torch.equal(got[2], dbeta)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,width,extra", [(3, 8199, 0), (3, 70001, 3), (2, 140000, 0), (4100, 8200, 0)])
+def test_long_rows_in_place(B, rows, width, extra, dtype):
+    # what a row has beyond a workgroup's registers is read again while the row is written over
+    x, dy, gamma, beta = make(rows, width, dtype, seed=8)
+    x, dy, ga, be = pitched(x, dtype, extra), pitched(dy, dtype, extra), gamma.cuda(), beta.cuda()
+    copy = lambda t: t.as_strided((rows, width + extra), (width + extra, 1)).clone()[:, :width]
+    y, mean, rstd = B.layer_norm_forward(x, ga, be)
+    a = copy(x)
+    B.layer_norm_forward(a, ga, be, y=a)
+    assert torch.equal(a, y)
+    dx, dgamma, dbeta = B.layer_norm_backward(x, dy, mean, rstd, ga)
+    for over in ("x", "dy"):
+        a, b = copy(x), copy(dy)
+        got = B.layer_norm_backward(a, b, mean, rstd, ga, dx=a if over == "x" else b)
+        assert torch.equal(got[0], dx) and torch.equal(got[1], dgamma) and torch.equal(got[2], dbeta)
